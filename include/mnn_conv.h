@@ -382,6 +382,107 @@ MNN_API int mnn_net_run(mnn_net_t net, const float* x, const float* const* w, co
 MNN_API int mnn_net_device_status(mnn_net_t net, void* stream, int* code, int* layer);
 MNN_API void mnn_net_destroy(mnn_net_t net);
 
+/*
+ * Matrix product over rows with its epilogue.  (The paper's engine runs fully connected layers as such products, Section 3.2;
+ * here it is what follows a network's feature map, and every projection of a token-wise model.)
+ *
+ *     s[m][n] = sum_k x[m][k] w[n][k] + bias[n]
+ *     y[m][n] = act(s)                        MNN_RESIDUAL_NONE
+ *     y[m][n] = act(s) + residual[m][n]       MNN_RESIDUAL_AFTER
+ *     y[m][n] = act(s + residual[m][n])       MNN_RESIDUAL_BEFORE
+ *
+ * x [M][ldx], w [N][ldw], bias [N] (NULL = zeros), residual [M][ldr] and y [M][ldy] are of ONE type (opts.type); within a row the
+ * elements are contiguous, rows may be any number of elements apart that is not smaller than their length.  Sums, bias,
+ * activation and residual are evaluated in fp32 and rounded once, at the store.  fp32 operands enter as TF32 halves (hi*hi +
+ * lo*hi + hi*lo, about 22 bits of mantissa); 16-bit operands as they are.  An infinity or NaN in x or w gives what the
+ * definition gives.  Pointers need the alignment of their element only; 16-byte aligned x and w with row strides of a multiple of
+ * 16 bytes are copied by TMA, others by a slower kernel.  y may be the residual itself (same pointer and stride) and must not
+ * overlap x, w or bias.  No operand is transformed ahead: one launch per run, for one row as for thousands.
+ * Rules on pointers, streams and errors as for the convolutions; the current device must be the device of `stream`.
+ */
+enum { MNN_TYPE_FP32 = 0, MNN_TYPE_BF16 = 1, MNN_TYPE_FP16 = 2 };
+/* GELU: v (1 + erf(v / sqrt 2)) / 2;  GELU_TANH: v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2;  SILU: v / (1 + e^-v) */
+enum { MNN_ACT_NONE = 0, MNN_ACT_RELU = 1, MNN_ACT_GELU = 2, MNN_ACT_GELU_TANH = 3, MNN_ACT_SILU = 4 };
+enum { MNN_RESIDUAL_NONE = 0, MNN_RESIDUAL_AFTER = 1, MNN_RESIDUAL_BEFORE = 2 };
+
+typedef struct mnn_linear_plan_s* mnn_linear_plan_t;   /* opaque host object */
+
+typedef struct {
+    int type;                        /* MNN_TYPE_* of every tensor */
+    int act;                         /* MNN_ACT_* */
+    int residual;                    /* MNN_RESIDUAL_* */
+    int reserved;
+    long long ldx, ldw, ldy, ldr;    /* elements between rows; 0 = dense */
+} mnn_linear_opts;
+
+typedef struct {
+    int M, N, K, type, act, residual;
+    int pair;                        /* 1: the kernel on pairs of SMs (256 features x 256 rows per work item) */
+    int copy;                        /* 1: rows are not 16-byte aligned and are fetched by warps instead of TMA */
+    int rows_per_item;               /* rows of x per work item; it has 128 features (256 on pairs) */
+    int split;                       /* CTAs of a cluster that share an item's K loop */
+    long long items;
+    long long workspace_bytes;       /* the status word */
+} mnn_linear_info;
+
+/* Plan one product (host only, needs no GPU); opts may be NULL = fp32, dense, no activation, no residual.  NULL on error:
+ * M, N and K must be positive and row strides at least the row length (MNN_EINVAL); tensors below 2^40 elements. */
+MNN_API mnn_linear_plan_t mnn_linear_plan(int M, int N, int K, const mnn_linear_opts* opts);
+MNN_API int mnn_linear_plan_query(mnn_linear_plan_t plan, mnn_linear_info* info);
+/* Hand over the caller-owned workspace (>= info.workspace_bytes, 1024-byte aligned) and clear its status word. */
+MNN_API int mnn_linear_set_workspace(mnn_linear_plan_t plan, void* workspace, long long bytes);
+/* One product on `stream`.  residual must be given exactly where the plan has one. */
+MNN_API int mnn_linear_run(mnn_linear_plan_t plan, const void* x, const void* w, const void* bias, const void* residual, void* y,
+                           void* stream);
+/* As mnn_conv_device_status. */
+MNN_API int mnn_linear_device_status(mnn_linear_plan_t plan, void* stream, int* code);
+MNN_API void mnn_linear_destroy(mnn_linear_plan_t plan);
+
+/*
+ * Sampling: one token per row of logits, from a given random number per row.  (The paper has no counterpart: it ends at the
+ * logits.)  For each row, with l its logits as fp32 and w_i = exp((l_i - max l) / temperature):
+ *   candidates    all i whose l_i is neither NaN nor -infinity; where +infinity occurs, those entries alone, with w = 1.
+ *                 No candidate at all: token -1, prob 0, probs 0.
+ *   temperature   not greater than 0 (or NaN): the largest candidate alone (of equals the lowest index).
+ *   order         falling l; of equals the lower index first.
+ *   top_k         k > 0: the first k candidates stay.
+ *   top_p         p < 1: of these a candidate stays while the mass (sum of w) before it is smaller than p times their mass; the
+ *                 first one always stays.
+ *   min_p         p > 0: of these stay those with w_i >= min(p, 1).
+ *   token         the lowest index i at which the sum of w over the candidates that stayed, up to and with i, exceeds u times
+ *                 their whole mass.  u in [0, 1); what lies outside counts as the nearest number inside, a NaN as 0.
+ *   prob          w of the token / mass of what stayed.
+ *   probs         the same for every i (0 for those that did not stay).
+ * Weights are evaluated in fp64 and summed as integers, so that a token does not depend on the order of additions.
+ *
+ * logits [rows][ld] of opts.type, temperature, top_p, min_p, u (float) and top_k (int) are DEVICE arrays of one value per row;
+ * each but u may be NULL (temperature 1, nothing cut).  token [rows] int, prob [rows] float or NULL, probs [rows][ld_probs]
+ * float or NULL.  Logits are read only; nothing behind a row's last entry is read or written.  One launch, no workspace.
+ */
+typedef struct mnn_sample_plan_s* mnn_sample_plan_t;   /* opaque host object */
+
+typedef struct {
+    int type;                        /* MNN_TYPE_* of the logits */
+    int reserved;
+    long long ld, ld_probs;          /* elements between rows; 0 = dense */
+} mnn_sample_opts;
+
+typedef struct {
+    int rows, vocab, type;
+    int ctas_per_row;                /* CTAs of the cluster that holds a row */
+    int threads;                     /* of a CTA */
+    int scale_log2;                  /* weights are integers in units of 2^-scale_log2 */
+} mnn_sample_info;
+
+#define MNN_SAMPLE_MAX_VOCAB (384 * 1024)
+/* Plan (host only); opts may be NULL = fp32, dense.  NULL on error: rows and vocab must be positive and row strides at least vocab
+ * (MNN_EINVAL); vocab at most MNN_SAMPLE_MAX_VOCAB and rows at most 2^27 (MNN_EUNSUPPORTED). */
+MNN_API mnn_sample_plan_t mnn_sample_plan(int rows, int vocab, const mnn_sample_opts* opts);
+MNN_API int mnn_sample_plan_query(mnn_sample_plan_t plan, mnn_sample_info* info);
+MNN_API int mnn_sample_run(mnn_sample_plan_t plan, const void* logits, const float* u, const float* temperature, const int* top_k,
+                           const float* top_p, const float* min_p, int* token, float* prob, float* probs, void* stream);
+MNN_API void mnn_sample_destroy(mnn_sample_plan_t plan);
+
 /* Self-test of the bounded waits every persistent kernel of the library relies on (no counterpart in the paper).
  * Launches one tiny kernel on `stream` that initialises a shared-memory barrier nobody ever arrives on and waits
  * on it with the library's bounded wait; the wait gives up after its limit (about one second) and the

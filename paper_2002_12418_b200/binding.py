@@ -31,8 +31,14 @@ EXPORTED = ["mnn_conv_plan", "mnn_conv_plan_ex", "mnn_conv_plan_rect", "mnn_conv
             "mnn_conv_profile", "mnn_conv_profile_read", "mnn_conv_destroy", "mnn_conv_run_static", "mnn_winograd_matrices", "mnn_accuracy_ppm", "mnn_strassen_rule", "mnn_wait_probe", "mnn_calibrate",
             "mnn_set_calibration", "mnn_get_calibration", "mnn_last_error",
             "mnn_net_plan", "mnn_net_query", "mnn_net_set_workspace", "mnn_net_prepare", "mnn_net_run",
-            "mnn_net_device_status", "mnn_net_destroy"]
+            "mnn_net_device_status", "mnn_net_destroy",
+            "mnn_linear_plan", "mnn_linear_plan_query", "mnn_linear_set_workspace", "mnn_linear_run", "mnn_linear_device_status",
+            "mnn_linear_destroy", "mnn_sample_plan", "mnn_sample_plan_query", "mnn_sample_run", "mnn_sample_destroy"]
 NET_MAX_LAYERS = 128
+TYPES = {"fp32": 0, "bf16": 1, "fp16": 2}                                                # MNN_TYPE_*
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}                      # MNN_ACT_*
+RESIDUALS = {"none": 0, "after": 1, "before": 2}                                         # MNN_RESIDUAL_*
+SAMPLE_MAX_VOCAB = 384 * 1024
 
 
 class ConvOpts(ctypes.Structure):
@@ -74,6 +80,26 @@ class NetInfo(ctypes.Structure):
                 ("algo", ctypes.c_int * NET_MAX_LAYERS), ("m", ctypes.c_int * NET_MAX_LAYERS),
                 ("operand", ctypes.c_int * NET_MAX_LAYERS), ("passes", ctypes.c_int * NET_MAX_LAYERS),
                 ("OH", ctypes.c_int * NET_MAX_LAYERS), ("OW", ctypes.c_int * NET_MAX_LAYERS)]
+
+
+class LinearOpts(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int), ("act", ctypes.c_int), ("residual", ctypes.c_int), ("reserved", ctypes.c_int),
+                ("ldx", ctypes.c_longlong), ("ldw", ctypes.c_longlong), ("ldy", ctypes.c_longlong), ("ldr", ctypes.c_longlong)]
+
+
+class LinearInfo(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int), ("N", ctypes.c_int), ("K", ctypes.c_int), ("type", ctypes.c_int), ("act", ctypes.c_int),
+                ("residual", ctypes.c_int), ("pair", ctypes.c_int), ("copy", ctypes.c_int), ("rows_per_item", ctypes.c_int),
+                ("split", ctypes.c_int), ("items", ctypes.c_longlong), ("workspace_bytes", ctypes.c_longlong)]
+
+
+class SampleOpts(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int), ("reserved", ctypes.c_int), ("ld", ctypes.c_longlong), ("ld_probs", ctypes.c_longlong)]
+
+
+class SampleInfo(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("vocab", ctypes.c_int), ("type", ctypes.c_int), ("ctas_per_row", ctypes.c_int),
+                ("threads", ctypes.c_int), ("scale_log2", ctypes.c_int)]
 
 
 class MnnError(RuntimeError):
@@ -147,6 +173,26 @@ def lib():
         L.mnn_net_device_status.restype = i
         L.mnn_net_destroy.argtypes = [p]
         L.mnn_net_destroy.restype = None
+        L.mnn_linear_plan.argtypes = [i, i, i, ctypes.POINTER(LinearOpts)]
+        L.mnn_linear_plan.restype = p
+        L.mnn_linear_plan_query.argtypes = [p, ctypes.POINTER(LinearInfo)]
+        L.mnn_linear_plan_query.restype = i
+        L.mnn_linear_set_workspace.argtypes = [p, p, ll]
+        L.mnn_linear_set_workspace.restype = i
+        L.mnn_linear_run.argtypes = [p] * 7
+        L.mnn_linear_run.restype = i
+        L.mnn_linear_device_status.argtypes = [p, p, ctypes.POINTER(i)]
+        L.mnn_linear_device_status.restype = i
+        L.mnn_linear_destroy.argtypes = [p]
+        L.mnn_linear_destroy.restype = None
+        L.mnn_sample_plan.argtypes = [i, i, ctypes.POINTER(SampleOpts)]
+        L.mnn_sample_plan.restype = p
+        L.mnn_sample_plan_query.argtypes = [p, ctypes.POINTER(SampleInfo)]
+        L.mnn_sample_plan_query.restype = i
+        L.mnn_sample_run.argtypes = [p] * 11
+        L.mnn_sample_run.restype = i
+        L.mnn_sample_destroy.argtypes = [p]
+        L.mnn_sample_destroy.restype = None
         L.mnn_last_error.argtypes = []
         L.mnn_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -334,6 +380,75 @@ def mnn_net_destroy(net) -> None:
     lib().mnn_net_destroy(net)
 
 
+def _choice(table, key, what):
+    if key not in table:
+        raise MnnError(MNN_EINVAL, "%s must be one of %s" % (what, ", ".join(table)))
+    return table[key]
+
+
+def make_linear_opts(dtype="fp32", act="none", residual="none", ldx=0, ldw=0, ldy=0, ldr=0) -> LinearOpts:
+    return LinearOpts(_choice(TYPES, dtype, "dtype"), _choice(ACTS, act, "act"), _choice(RESIDUALS, residual, "residual"), 0,
+                      ldx, ldw, ldy, ldr)
+
+
+def mnn_linear_plan(M, N, K, opts: LinearOpts | None):
+    h = lib().mnn_linear_plan(M, N, K, ctypes.byref(opts) if opts is not None else None)
+    if not h:
+        raise MnnError(MNN_EINVAL, mnn_last_error())
+    return h
+
+
+def mnn_linear_plan_query(plan) -> LinearInfo:
+    info = LinearInfo()
+    _check(lib().mnn_linear_plan_query(plan, ctypes.byref(info)))
+    return info
+
+
+def mnn_linear_set_workspace(plan, ptr: int, nbytes: int) -> None:
+    _check(lib().mnn_linear_set_workspace(plan, ptr, nbytes))
+
+
+def mnn_linear_run(plan, x_ptr, w_ptr, bias_ptr, residual_ptr, y_ptr, stream: int) -> None:
+    _check(lib().mnn_linear_run(plan, x_ptr, w_ptr, bias_ptr, residual_ptr, y_ptr, stream))
+
+
+def mnn_linear_device_status(plan, stream: int) -> int:
+    code = ctypes.c_int(0)
+    _check(lib().mnn_linear_device_status(plan, stream, ctypes.byref(code)))
+    return code.value
+
+
+def mnn_linear_destroy(plan) -> None:
+    lib().mnn_linear_destroy(plan)
+
+
+def make_sample_opts(dtype="fp32", ld=0, ld_probs=0) -> SampleOpts:
+    return SampleOpts(_choice(TYPES, dtype, "dtype"), 0, ld, ld_probs)
+
+
+def mnn_sample_plan(rows, vocab, opts: SampleOpts | None):
+    h = lib().mnn_sample_plan(rows, vocab, ctypes.byref(opts) if opts is not None else None)
+    if not h:
+        raise MnnError(MNN_EINVAL, mnn_last_error())
+    return h
+
+
+def mnn_sample_plan_query(plan) -> SampleInfo:
+    info = SampleInfo()
+    _check(lib().mnn_sample_plan_query(plan, ctypes.byref(info)))
+    return info
+
+
+def mnn_sample_run(plan, logits_ptr, u_ptr, temperature_ptr, top_k_ptr, top_p_ptr, min_p_ptr, token_ptr, prob_ptr, probs_ptr,
+                   stream: int) -> None:
+    _check(lib().mnn_sample_run(plan, logits_ptr, u_ptr, temperature_ptr, top_k_ptr, top_p_ptr, min_p_ptr, token_ptr, prob_ptr,
+                                probs_ptr, stream))
+
+
+def mnn_sample_destroy(plan) -> None:
+    lib().mnn_sample_destroy(plan)
+
+
 def _raw_stream(device):
     """A callable that returns the handle of torch's current stream on `device`: torch's own lookup of the handle where the device
     is named by its index, without the Stream object that torch.cuda.current_stream builds."""
@@ -457,3 +572,129 @@ class ConvLayerRunner:
             self.close()
         except Exception:
             pass
+
+
+class _RowRunner:
+    """What the runners over rows share: torch's stream, the device of a launch, and checks of tensors (the C ABI sees pointers
+    only, so a tensor of another type or shape has to be refused here)."""
+
+    def __init__(self, dtype, device):
+        import torch
+        self.torch = torch
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        _choice(TYPES, dtype, "dtype")
+        self.dtype = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+        self._raw_stream = _raw_stream(self.device)
+
+    def stream(self) -> int:
+        return self._raw_stream()
+
+    def _rows(self, t, shape, ld, what, dtype=None):
+        """The address of a tensor of `shape` whose rows are ld elements apart."""
+        if t.dtype is not (dtype or self.dtype) or t.device != self.device or t.shape != shape:
+            raise MnnError(MNN_EINVAL, "%s must be a %s tensor of shape %s on %s" % (what, dtype or self.dtype, tuple(shape), self.device))
+        if shape[1] > 1 and t.stride(1) != 1 or shape[0] > 1 and t.stride(0) != ld:
+            raise MnnError(MNN_EINVAL, "rows of %s must be contiguous and %d elements apart" % (what, ld))
+        return t.data_ptr()
+
+    def _vector(self, t, shape, what, dtype):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.device != self.device or t.shape != shape or not t.is_contiguous():
+            raise MnnError(MNN_EINVAL, "%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), self.device))
+        return t.data_ptr()
+
+    def _launch(self, call, *args):
+        """The library's call with this runner's device as the current one."""
+        torch = self.torch
+        if torch.cuda.current_device() == self.device.index:
+            rc = call(self.plan, *args, self._raw_stream())
+        else:
+            with torch.cuda.device(self.device):
+                rc = call(self.plan, *args, self._raw_stream())
+        if rc != MNN_OK:
+            _check(rc)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class LinearRunner(_RowRunner):
+    """y = act(x w^T + bias) with a residual (``mnn_linear_plan`` / ``mnn_linear_run``): x [M, K], w [N, K], bias [N],
+    residual and y [M, N], all of one type ("fp32", "bf16", "fp16").  Row strides that differ from dense ones are planned
+    (ldx, ldw, ldy, ldr)."""
+
+    def __init__(self, M, N, K, dtype="fp32", act="none", residual="none", ldx=0, ldw=0, ldy=0, ldr=0, device="cuda:0"):
+        super().__init__(dtype, device)
+        torch = self.torch
+        self.plan = mnn_linear_plan(M, N, K, make_linear_opts(dtype, act, residual, ldx, ldw, ldy, ldr))
+        self.info = mnn_linear_plan_query(self.plan)
+        self._x, self._w, self._y, self._n = torch.Size((M, K)), torch.Size((N, K)), torch.Size((M, N)), torch.Size((N,))
+        self._ldx, self._ldw, self._ldy, self._ldr = ldx or K, ldw or K, ldy or N, ldr or N
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(self.info.workspace_bytes + 1024, dtype=torch.uint8, device=self.device)
+            self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
+            mnn_linear_set_workspace(self.plan, self._ws_ptr, self.info.workspace_bytes)
+
+    def run(self, x, w, bias=None, residual=None, y=None):
+        if y is None:
+            if self._ldy == self._y[1]:
+                y = self.torch.empty(self._y, dtype=self.dtype, device=self.device)
+            else:
+                y = self.torch.empty((self._y[0], self._ldy), dtype=self.dtype, device=self.device)[:, :self._y[1]]
+        self._launch(_lib.mnn_linear_run, self._rows(x, self._x, self._ldx, "x"), self._rows(w, self._w, self._ldw, "w"),
+                     self._vector(bias, self._n, "bias", self.dtype),
+                     self._rows(residual, self._y, self._ldr, "residual") if residual is not None else None,
+                     self._rows(y, self._y, self._ldy, "y"))
+        return y
+
+    def device_status(self) -> int:
+        return mnn_linear_device_status(self.plan, self.stream())
+
+    def close(self) -> None:
+        if self.plan:
+            mnn_linear_destroy(self.plan)
+            self.plan = None
+
+
+class SampleRunner(_RowRunner):
+    """One token per row of logits [rows, vocab] (``mnn_sample_plan`` / ``mnn_sample_run``).  ``run`` returns (token int32, prob
+    fp32, probs fp32 or None); u, temperature, top_p, min_p are fp32 and top_k int32 tensors of one value per row."""
+
+    def __init__(self, rows, vocab, dtype="fp32", ld=0, device="cuda:0"):
+        super().__init__(dtype, device)
+        self.plan = mnn_sample_plan(rows, vocab, make_sample_opts(dtype, ld))
+        self.info = mnn_sample_plan_query(self.plan)
+        self._logits, self._n, self._ld = self.torch.Size((rows, vocab)), self.torch.Size((rows,)), ld or vocab
+
+    def run(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, probs=False, token=None, prob=None):
+        """probs: True for the whole filtered distribution too, or the tensor to write it to."""
+        torch = self.torch
+        f = torch.float32
+        if u is None:
+            raise MnnError(MNN_EINVAL, "u is required")
+        if token is None:
+            token = torch.empty(self._n, dtype=torch.int32, device=self.device)
+        if prob is None:
+            prob = torch.empty(self._n, dtype=f, device=self.device)
+        if probs is True:
+            probs = torch.empty(self._logits, dtype=f, device=self.device)
+        elif probs is False:
+            probs = None
+        n = self._n
+        self._launch(_lib.mnn_sample_run, self._rows(logits, self._logits, self._ld, "logits"), self._vector(u, n, "u", f),
+                     self._vector(temperature, n, "temperature", f), self._vector(top_k, n, "top_k", torch.int32),
+                     self._vector(top_p, n, "top_p", f), self._vector(min_p, n, "min_p", f),
+                     self._vector(token, n, "token", torch.int32), self._vector(prob, n, "prob", f),
+                     self._rows(probs, self._logits, self._logits[1], "probs", f) if probs is not None else None)
+        return token, prob, probs
+
+    def close(self) -> None:
+        if self.plan:
+            mnn_sample_destroy(self.plan)
+            self.plan = None

@@ -14,6 +14,7 @@
 #include "implicit_gemm.h"
 #include "contract_pair.h"
 #include "contract_umma.h"
+#include "errors.h"
 #include "kernels.h"
 #include "line_conv.h"
 #include "line_wino.h"
@@ -46,6 +47,9 @@ long long align_up(long long v, long long a) { return (v + a - 1) / a * a; }
 constexpr long long kStatusBytes = 1024;   // head of the workspace: device status word
 
 }  // namespace
+
+int mnnb::report_error(int code, const char* why) { return fail(code, why); }
+int mnnb::report_cuda_error(cudaError_t e, const char* where) { return fail_cuda(e, where); }
 
 struct mnn_conv_plan_s {
     LayerShape s;

@@ -1,0 +1,582 @@
+// Matrix product over rows with its epilogue, y = act(x w^T + bias) with a residual, on single SMs:
+//     s[m][n] = sum_k x[m][k] w[n][k]
+// The same persistent, warp-specialised structure as the contraction of the convolutions (contract_umma.cu), with the roles of
+// the two operands turned round: the MMA "M" dimension (128 lanes of tensor memory) is the output feature n, "N" (bm columns, 16
+// to 256) the row m of x.  One kernel then serves a single row as well as thousands: with few rows nearly all bytes are weights,
+// which stream through the 128-row side at full tile width, and only the columns shrink.  In the epilogue the 32 lanes of a warp
+// are 32 consecutive features of one row: stores, residual and bias are contiguous whatever the row strides are.
+//
+// With few work items a cluster of `split` CTAs shares each item's K loop and adds its partial sums in rank order through
+// distributed shared memory (cluster.cuh): deterministic, one launch, no workspace.
+//
+// 16-bit operands go to the tensor core as they are.  fp32 operands are cut in two: the tensor core reads the high 19 bits
+// (TF32, dropping the low 13), and `converter` warps write lo = v - trunc(v), exact in fp32, beside each tile; hi*hi goes to one
+// accumulator, lo*hi + hi*lo to another (the dropped lo*lo is 2^-22 of a product).  The tensor core's own additions cut their
+// result off instead of rounding it, which over a long K loop grows to a bias of about 2^-25 per step; so after every kSegment
+// blocks of K both accumulators are added to fp32 registers, which round.  Sums that this leaves without a finite value
+// (an infinity's low half is no number) are taken again by their thread, term by term in fp32.
+//
+// Operands whose rows do not start on 16-byte boundaries cannot be copied by TMA: `copier` warps read aligned 16-byte pieces,
+// shift neighbours together and write the swizzled tile themselves.
+#include "cluster.cuh"
+#include "linear_epilogue.cuh"
+#include "kernels.h"
+#include "umma.cuh"
+
+namespace mnnb {
+
+namespace {
+
+constexpr int kTileF = 128;              // features per work item
+constexpr int kEpiWarps = 8;
+constexpr int kLinearSmem = 200 * 1024;
+constexpr int kLinearMaxStages = 10;
+constexpr int kSegment = 4;              // fp32: blocks of 32 elements of K between additions to the registers
+constexpr int kErrProducer = 51, kErrMmaFull = 52, kErrMmaTmem = 53, kErrEpilogue = 54, kErrAux = 55;   // status codes
+
+struct LinearParams {
+    int M, N, K, bm, n_fblocks, n_mblocks, k_blocks, stages, tmem_cols, split;
+    long long items;
+    const void *x, *w;
+    long long ldx, ldw;
+    LinearEpilogue epi;
+    int* status;
+};
+
+template <int TYPE, bool COPY>
+struct Roles {
+    // copier or converter warps; four where the epilogue's sums need the registers
+    static constexpr int kAux = TYPE == MNN_TYPE_FP32 ? 4 : COPY ? 8 : 0;
+    static constexpr int kThreads = 64 + 32 * (kEpiWarps + kAux);
+};
+
+__device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// lo = v - trunc(v) of the four values; an infinity's or NaN's is 0
+__device__ __forceinline__ float low_half(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    return (b & 0x7f800000u) == 0x7f800000u ? 0.0f : v - __uint_as_float(b & 0xffffe000u);
+}
+__device__ __forceinline__ float4 low_half(float4 v) { return make_float4(low_half(v.x), low_half(v.y), low_half(v.z), low_half(v.w)); }
+
+// The 16 bytes at `at` of the tensor [begin, end), of which the first `valid` are wanted, the others zero.
+template <int EB>
+__device__ __forceinline__ uint4 load_piece(const char* at, int valid, const char* begin, const char* end)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+    const char* lo = at - (a & 15u);
+    if (valid >= 16 && (a & 15u) == 0) return __ldg(reinterpret_cast<const uint4*>(at));
+    if (valid >= 16 && lo >= begin && lo + 32 <= end) {
+        const uint4 p = __ldg(reinterpret_cast<const uint4*>(lo)), q = __ldg(reinterpret_cast<const uint4*>(lo) + 1);
+        uint32_t u0 = p.x, u1 = p.y, u2 = p.z, u3 = p.w, u4 = q.x, u5 = q.y, u6 = q.z;
+        if (a & 8u) { u0 = u2; u1 = u3; u2 = u4; u3 = u5; u4 = u6; u5 = q.w; u6 = 0; }
+        if (a & 4u) { u0 = u1; u1 = u2; u2 = u3; u3 = u4; u4 = u5; }
+        if (EB == 2 && (a & 2u)) {
+            u0 = __funnelshift_r(u0, u1, 16);
+            u1 = __funnelshift_r(u1, u2, 16);
+            u2 = __funnelshift_r(u2, u3, 16);
+            u3 = __funnelshift_r(u3, u4, 16);
+        }
+        return make_uint4(u0, u1, u2, u3);
+    }
+    uint32_t u[4] = {0, 0, 0, 0};
+    if (EB == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j * 4 < valid) u[j] = __ldg(reinterpret_cast<const uint32_t*>(at) + j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j * 2 < valid) u[j >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(at) + j) << ((j & 1) * 16);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// TYPE: MNN_TYPE_*; COPY: operands fetched by copier warps; SPLIT: clusters share K loops; KB: blocks of K (128 bytes a row) per
+// stage.
+template <int TYPE, bool COPY, bool SPLIT, int KB>
+__global__ void __launch_bounds__(Roles<TYPE, COPY>::kThreads, 1)
+linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, LinearParams p)
+{
+    constexpr bool F32 = TYPE == MNN_TYPE_FP32;
+    constexpr int kAux = Roles<TYPE, COPY>::kAux;
+    constexpr int EB = F32 ? 4 : 2;
+    constexpr int kBlockElems = 128 / EB;
+    static_assert(KB == 1 || (!F32 && !COPY), "only 16-bit stages copied by TMA hold two blocks");
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full_bar[kLinearMaxStages];      // operands landed (or written by the copiers)
+    __shared__ __align__(8) uint64_t low_bar[kLinearMaxStages];       // fp32 by TMA: low halves written
+    __shared__ __align__(8) uint64_t empty_bar[kLinearMaxStages];
+    __shared__ __align__(8) uint64_t tfull_bar[2];
+    __shared__ __align__(8) uint64_t tempty_bar[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t a_bytes = kTileF * 128, b_bytes = (uint32_t)p.bm * 128;
+    // stage: [A] x KB [B] x KB, for fp32 followed by [A low][B low]
+    const uint32_t raw_bytes = (a_bytes + b_bytes) * KB, stage_bytes = raw_bytes * (F32 ? 2 : 1), off_b = a_bytes * KB;
+    volatile int* abortp = &abort_flag;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&full_bar[s]), COPY ? kAux : 1);
+            ptx::mbar_init(ptx::smem_u32(&low_bar[s]), kAux ? kAux : 1);
+            ptx::mbar_init(ptx::smem_u32(&empty_bar[s]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&tfull_bar[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&tempty_bar[s]), kEpiWarps);
+        }
+        abort_flag = 0;
+        ptx::fence_barrier_init();
+        if (!COPY) {
+            ptx::prefetch_tensormap(&map_x);
+            ptx::prefetch_tensormap(&map_w);
+        }
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), (uint32_t)p.tmem_cols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem_base = tmem_slot;
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+
+    const uint32_t rank = SPLIT ? ptx::cluster_ctarank() : 0u;
+    const long long first_item = SPLIT ? blockIdx.x / (unsigned)p.split : blockIdx.x;
+    const long long item_step = SPLIT ? gridDim.x / (unsigned)p.split : gridDim.x;
+    const int kb0 = SPLIT ? (int)((long long)p.k_blocks * (int)rank / p.split) : 0;
+    const int kb1 = SPLIT ? (int)((long long)p.k_blocks * ((int)rank + 1) / p.split) : p.k_blocks;
+    auto failed = [&](int code) {                      // called by one lane
+        if (!*abortp) atomicCAS(p.status, 0, code);
+        *abortp = 1;
+    };
+
+    if (warp == 0) {
+        if (!COPY) {
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            for (long long item = first_item; item < p.items && ok; item += item_step) {
+                int fb, mb;
+                linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!ptx::mbar_wait_warp(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp)) {
+                        if (lane == 0) failed(kErrProducer);
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t bar = ptx::smem_u32(&full_bar[stage]), sbase = smem_base + stage * stage_bytes;
+                    if (ptx::elect_one()) {
+                        ptx::mbar_expect_tx(bar, raw_bytes);
+#pragma unroll
+                        for (int h = 0; h < KB; ++h) {
+                            const int ke = (kb * KB + h) * kBlockElems;
+                            ptx::tma_load_2d(sbase + h * a_bytes, &map_w, bar, ke, fb * kTileF);
+                            ptx::tma_load_2d(sbase + off_b + h * b_bytes, &map_x, bar, ke, mb * p.bm);
+                        }
+                    }
+                    if (++stage == (uint32_t)p.stages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // instruction format: 2 = TF32, 1 = BF16, 0 = FP16
+        const uint32_t idesc = ptx::mma_idesc(F32 ? 2 : TYPE == MNN_TYPE_BF16 ? 1 : 0, kTileF, p.bm);
+        constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);       // 8-row groups 1024 bytes apart, 128-byte swizzle
+        uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+        bool ok = true;
+        const uint32_t a_lo0 = ((smem_base & 0x3FFFFu) >> 4) | (1u << 16);
+        for (long long item = first_item; item < p.items && ok; item += item_step) {
+            for (int seg = kb0; seg < kb1 && ok; seg += F32 ? kSegment : kb1 - kb0) {
+                if (!ptx::mbar_wait_warp(ptx::smem_u32(&tempty_bar[acc]), acc_phase ^ 1u, abortp)) {
+                    if (lane == 0) failed(kErrMmaTmem);
+                    ok = false;
+                    break;
+                }
+                ptx::tc_fence_after();
+                const uint32_t d_main = tmem_base + acc * (uint32_t)(p.bm * (F32 ? 2 : 1)), d_cross = d_main + (uint32_t)p.bm;
+                const int seg_end = F32 ? min(seg + kSegment, kb1) : kb1;
+                uint32_t accumulate = 0;
+                for (int kb = seg; kb < seg_end; ++kb) {
+                    if (!ptx::mbar_wait_warp(ptx::smem_u32(F32 && !COPY ? &low_bar[stage] : &full_bar[stage]), phase, abortp)) {
+                        if (lane == 0) failed(kErrMmaFull);
+                        ok = false;
+                        break;
+                    }
+                    if (COPY || F32) ptx::tc_fence_after();
+                    const uint32_t a0 = a_lo0 + stage * (stage_bytes >> 4), b0 = a0 + (off_b >> 4);
+                    if (ptx::elect_one()) {
+#pragma unroll
+                        for (int h = 0; h < KB; ++h)
+#pragma unroll
+                            for (int ks = 0; ks < 4; ++ks) {
+                                const uint32_t a = a0 + h * (a_bytes >> 4) + ks * 2, b = b0 + h * (b_bytes >> 4) + ks * 2;
+                                const uint32_t go = h || ks ? 1u : accumulate;
+                                ptx::mma_lo<F32 ? 0 : 1>(d_main, a, b, kDescHi, idesc, go);
+                                if (F32) {
+                                    ptx::mma_lo<0>(d_cross, a + (raw_bytes >> 4), b, kDescHi, idesc, go);
+                                    ptx::mma_lo<0>(d_cross, a, b + (raw_bytes >> 4), kDescHi, idesc, 1u);
+                                }
+                            }
+                        ptx::mma_commit(ptx::smem_u32(&empty_bar[stage]));
+                    }
+                    accumulate = 1u;
+                    if (++stage == (uint32_t)p.stages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                if (ptx::elect_one()) ptx::mma_commit(ptx::smem_u32(&tfull_bar[acc]));
+                acc ^= 1u;
+                if (acc == 0) acc_phase ^= 1u;
+            }
+        }
+    } else if (warp < 2 + kEpiWarps) {
+        const int q = warp & 3;                        // tensor-memory lane quarter this warp may read
+        const int part = (warp - 2) >> 2;              // which half of the columns
+        const int n_chunks = p.bm >> 4, per_part = (n_chunks + 1) >> 1;
+        const int ch0 = part * per_part, ch1 = min(ch0 + per_part, n_chunks);
+        uint32_t acc = 0, acc_phase = 0;
+        bool ok = true;
+        auto wait_acc = [&]() {
+            int got = 1;
+            if (lane == 0) got = ptx::mbar_wait_relaxed(ptx::smem_u32(&tfull_bar[acc]), acc_phase, abortp) ? 1 : 0;
+            got = __shfl_sync(0xffffffffu, got, 0);
+            if (!got && lane == 0) failed(kErrEpilogue);
+            ptx::tc_fence_after();
+            return got != 0;
+        };
+        auto release_acc = [&]() {
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&tempty_bar[acc]));
+            acc ^= 1u;
+            if (acc == 0) acc_phase ^= 1u;
+        };
+        for (long long item = first_item; item < p.items && ok; item += item_step) {
+            int fb, mb;
+            linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
+            const int n = fb * kTileF + q * 32 + lane;
+            const bool n_ok = n < p.N;
+            const long long m_item = (long long)mb * p.bm;
+            const float bias = SPLIT ? 0.0f : linear_bias<TYPE>(p.epi, n, n_ok);
+            // the finished sums of one chunk of 16 rows
+            auto emit = [&](float (&s)[16], int ch, LinearStore<TYPE, 16>& out) {
+                if (SPLIT) {                            // partial sums over the operand slots, which nothing uses any more
+                    const uint32_t red = smem_base + (uint32_t)(ch * 16 * 128 + q * 32 + lane) * 4u;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(red + j * 512), "f"(s[j]) : "memory");
+                    return;
+                }
+                const long long m0 = m_item + ch * 16;
+                const int rows = (int)min(16ll, p.M - m0);
+                if (F32 && n_ok) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j < rows && !isfinite(s[j])) {
+                            const float *xr = static_cast<const float*>(p.x) + (m0 + j) * p.ldx, *wr = static_cast<const float*>(p.w) + (long long)n * p.ldw;
+                            float t = 0.0f;
+                            for (int k = 0; k < p.K; ++k) t = fmaf(xr[k], wr[k], t);
+                            s[j] = t;
+                        }
+                }
+                out.store(p.epi, s, bias, m0, rows, n, n_ok);
+            };
+            if (F32) {
+                float sum[4][16];                       // at most 64 of the 128 columns belong to this warp
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] = 0.0f;
+                for (int seg = kb0; seg < kb1; seg += kSegment) {
+                    if (!wait_acc()) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * (uint32_t)(p.bm * 2);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (ch0 + c < ch1) {
+                            uint32_t va[16], vb[16];
+                            ptx::tmem_ld16(taddr + (uint32_t)((ch0 + c) * 16), va);
+                            ptx::tmem_ld16(taddr + (uint32_t)(p.bm + (ch0 + c) * 16), vb);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sum[c][j] += __uint_as_float(va[j]) + __uint_as_float(vb[j]);
+                        }
+                    release_acc();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (ch0 + c < ch1) {
+                        LinearStore<TYPE, 16> out;
+                        const long long m0 = m_item + (ch0 + c) * 16;
+                        if (!SPLIT) out.fetch(p.epi, m0, (int)min(16ll, p.M - m0), n, n_ok);
+                        emit(sum[c], ch0 + c, out);
+                    }
+            } else {
+                LinearStore<TYPE, 16> out;
+                auto fetch = [&](int ch) {
+                    const long long m0 = m_item + ch * 16;
+                    if (!SPLIT && ch < ch1) out.fetch(p.epi, m0, (int)min(16ll, p.M - m0), n, n_ok);
+                };
+                fetch(ch0);
+                if (!wait_acc()) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * (uint32_t)p.bm;
+                uint32_t v[16];
+                if (ch0 < ch1) ptx::tmem_ld16(taddr + (uint32_t)(ch0 * 16), v);
+                for (int ch = ch0; ch < ch1; ++ch) {
+                    ptx::tmem_ld_wait();
+                    float s[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) s[j] = __uint_as_float(v[j]);
+                    LinearStore<TYPE, 16> now = out;
+                    if (ch + 1 < ch1) ptx::tmem_ld16(taddr + (uint32_t)((ch + 1) * 16), v);
+                    fetch(ch + 1);
+                    emit(s, ch, now);
+                }
+                release_acc();
+            }
+        }
+    } else if (COPY) {
+        // copiers: a row's eight 16-byte pieces by eight lanes, four rows at a time by each warp
+        const int w = warp - 2 - kEpiWarps, piece = lane & 7, sub = lane >> 3;
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        uint8_t* const generic_base = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+        const char *xb = static_cast<const char*>(p.x), *wb = static_cast<const char*>(p.w);
+        const char *xe = xb + ((p.M - 1) * p.ldx + p.K) * EB, *we = wb + ((p.N - 1) * p.ldw + p.K) * EB;
+        for (long long item = first_item; item < p.items && ok; item += item_step) {
+            int fb, mb;
+            linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                int got = 1;
+                if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp) ? 1 : 0;
+                got = __shfl_sync(0xffffffffu, got, 0);
+                if (!got) {
+                    if (lane == 0) failed(kErrAux);
+                    ok = false;
+                    break;
+                }
+                uint8_t* const sbase = generic_base + stage * stage_bytes;
+                const int k0 = kb * kBlockElems + piece * (16 / EB);
+                const int valid = min(16, (p.K - k0) * EB);
+                auto rows_of = [&](const char* base, const char* end, long long ld, int row0, int total, int rows, uint8_t* tile) {
+#pragma unroll 4
+                    for (int r = w * 4 + sub; r < rows; r += 4 * kAux) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (row0 + r < total && valid > 0) v = load_piece<EB>(base + ((long long)(row0 + r) * ld + k0) * EB, valid, base, end);
+                        const uint32_t at = (uint32_t)r * 128u + (uint32_t)((piece ^ (r & 7)) << 4);
+                        *reinterpret_cast<uint4*>(tile + at) = v;
+                        if (F32) *reinterpret_cast<float4*>(tile + raw_bytes + at) = low_half(make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)));
+                    }
+                };
+                rows_of(wb, we, p.ldw, fb * kTileF, p.N, kTileF, sbase);
+                rows_of(xb, xe, p.ldx, mb * p.bm, p.M, p.bm, sbase + off_b);
+                fence_proxy_async_smem();                      // the tensor core reads these through the async proxy
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&full_bar[stage]));
+                if (++stage == (uint32_t)p.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+        }
+    } else if (F32) {
+        // converters: the low halves of both tiles, in the same (swizzled) places
+        const int t = threadIdx.x - 32 * (2 + kEpiWarps);
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        uint8_t* const generic_base = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+        for (long long item = first_item; item < p.items && ok; item += item_step)
+            for (int kb = kb0; kb < kb1; ++kb) {
+                int got = 1;
+                if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&full_bar[stage]), phase, abortp) ? 1 : 0;
+                got = __shfl_sync(0xffffffffu, got, 0);
+                if (!got) {
+                    if (lane == 0) failed(kErrAux);
+                    ok = false;
+                    break;
+                }
+                const float4* const raw = reinterpret_cast<const float4*>(generic_base + stage * stage_bytes);
+                float4* const low = reinterpret_cast<float4*>(generic_base + stage * stage_bytes + raw_bytes);
+                const int count = (int)(raw_bytes >> 4);
+#pragma unroll 4
+                for (int i = t; i < count; i += 32 * kAux) low[i] = low_half(raw[i]);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&low_bar[stage]));
+                if (++stage == (uint32_t)p.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+    }
+
+    if (SPLIT) {
+        __syncwarp();
+        ptx::cluster_sync_all();
+        if (warp >= 2 && warp < 2 + kEpiWarps && !*abortp && first_item < p.items) {
+            int fb, mb;
+            linear_item(first_item, p.n_fblocks, p.n_mblocks, &fb, &mb);
+            const int row = (warp & 3) * 32 + lane, n = fb * kTileF + row;
+            const bool n_ok = n < p.N;
+            const float bias = linear_bias<TYPE>(p.epi, n, n_ok);
+            if (n_ok)
+                ptx::cluster_reduce_columns(smem_base, p.bm, rank, p.split, row, (warp - 2) >> 2, kEpiWarps >> 2, [&](int c, float sum) {
+                    const long long m = (long long)mb * p.bm + c;
+                    if (m >= p.M) return;
+                    if (F32 && !isfinite(sum)) {
+                        const float *xr = static_cast<const float*>(p.x) + m * p.ldx, *wr = static_cast<const float*>(p.w) + (long long)n * p.ldw;
+                        sum = 0.0f;
+                        for (int k = 0; k < p.K; ++k) sum = fmaf(xr[k], wr[k], sum);
+                    }
+                    LinearStore<TYPE, 1> out;
+                    out.fetch(p.epi, m, 1, n, true);
+                    float s[1] = {sum};
+                    out.store(p.epi, s, bias, m, 1, n, true);
+                });
+        }
+        __syncwarp();
+        ptx::cluster_sync_all();                           // nobody leaves while its partial sums are being read
+    }
+
+    // Teardown.  After an aborted run give copies still in flight time to land before shared memory is released.
+    if (*abortp) __nanosleep(200000);
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+    }
+}
+
+template <int TYPE, bool COPY, bool SPLIT, int KB>
+cudaError_t run_variant(const LinearTiling& t, LinearParams& p, int num_sms, const CUtensorMap& mx, const CUtensorMap& mw, cudaStream_t stream)
+{
+    constexpr bool F32 = TYPE == MNN_TYPE_FP32;
+    static unsigned long long done = 0;
+    auto kern = linear_kernel<TYPE, COPY, SPLIT, KB>;
+    cudaError_t e = allow_smem_once(reinterpret_cast<const void*>(kern), kLinearSmem, &done);
+    if (e != cudaSuccess) return e;
+    const int stage_bytes = (kTileF + p.bm) * 128 * KB * (F32 ? 2 : 1);
+    p.stages = (kLinearSmem - 1024) / stage_bytes;
+    if (p.stages > kLinearMaxStages) p.stages = kLinearMaxStages;
+    p.k_blocks = (p.K + 128 / (F32 ? 4 : 2) * KB - 1) / (128 / (F32 ? 4 : 2) * KB);
+    p.tmem_cols = 32;
+    while (p.tmem_cols < p.bm * (F32 ? 4 : 2)) p.tmem_cols *= 2;
+    const dim3 block(Roles<TYPE, COPY>::kThreads);
+    // the full budget of shared memory, so that one CTA at most is resident per SM: a second one could block in its
+    // tensor-memory allocation
+    if (SPLIT) return launch_cluster(t.split, kern, dim3((unsigned)(t.items * t.split)), block, (size_t)kLinearSmem, stream, mx, mw, p);
+    const long long grid = t.items < num_sms ? t.items : num_sms;
+    return launch_overlapped(kern, dim3((unsigned)grid), block, (size_t)kLinearSmem, stream, mx, mw, p);
+}
+
+template <int TYPE, int KB>
+cudaError_t run_type(const LinearTiling& t, LinearParams& p, int num_sms, const CUtensorMap& mx, const CUtensorMap& mw, cudaStream_t stream)
+{
+    if (t.copy) return t.split > 1 ? run_variant<TYPE, true, true, 1>(t, p, num_sms, mx, mw, stream) : run_variant<TYPE, true, false, 1>(t, p, num_sms, mx, mw, stream);
+    return t.split > 1 ? run_variant<TYPE, false, true, KB>(t, p, num_sms, mx, mw, stream) : run_variant<TYPE, false, false, KB>(t, p, num_sms, mx, mw, stream);
+}
+
+}  // namespace
+
+cudaError_t allow_smem_once(const void* kern, int bytes, unsigned long long* done)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev < 64 && (__atomic_load_n(done, __ATOMIC_ACQUIRE) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) __atomic_fetch_or(done, bit, __ATOMIC_RELEASE);
+    return e;
+}
+
+LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
+{
+    const bool f32 = s.type == MNN_TYPE_FP32;
+    const int eb = f32 ? 4 : 2;
+    LinearTiling t = {};
+    t.copy = unaligned || (s.ldx * eb) % 16 != 0 || (s.ldw * eb) % 16 != 0;
+    // Estimated clocks: waves of CTAs, each its share of K blocks at the slower of the tensor core (4096 multiply-adds of 16 bits
+    // a clock; TF32 half of that, three products) and the delivery of the tiles (about 48 bytes a clock and SM), plus start and end.
+    const long long fblocks = (s.N + kTileF - 1) / kTileF, kblocks = ((long long)s.K * eb + 127) / 128;
+    double best = 0;
+    for (int bm = 16; bm <= (f32 ? 128 : 256); bm *= 2) {
+        if (bm > 16 && bm / 2 >= s.M) break;
+        const long long items = fblocks * ((s.M + bm - 1) / bm);
+        for (int split = 1; split <= 8; split *= 2) {
+            if (split > 1 && (items * split > num_sms || kblocks < 2 * split)) break;
+            const double mma = f32 ? 6.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.copy ? 16.0 : 48.0);
+            const long long waves = (items * split + num_sms - 1) / num_sms;
+            const double clocks = waves * ((kblocks + split - 1) / split * (mma > load ? mma : load)) + 1500.0 + 8.0 * bm + (split > 1 ? 1200.0 + 6.0 * bm : 0.0);
+            if (best == 0 || clocks < best) {
+                best = clocks;
+                t.bm = bm;
+                t.split = split;
+                t.items = items;
+            }
+        }
+    }
+    // pairs of SMs: half the rows of x per CTA, so that the tensor core and not the delivery decides
+    if (!f32 && !t.copy) {
+        const long long items = ((s.N + 255) / 256) * (long long)((s.M + 255) / 256), pairs = num_sms / 2;
+        const double clocks = (double)((items + pairs - 1) / pairs) * (kblocks * 660.0) + 3500.0;
+        if (clocks < best) {
+            t.pair = 1;
+            t.bm = 256;
+            t.split = 1;
+            t.items = items;
+        }
+    }
+    return t;
+}
+
+cudaError_t launch_linear(const LinearShape& s, const LinearTiling& t, int num_sms, const void* x, const void* w,
+                          const LinearEpilogue& epi, int* status, cudaStream_t stream, const char** why)
+{
+    LinearParams p = {};
+    p.M = s.M; p.N = s.N; p.K = s.K;
+    p.bm = t.bm;
+    p.n_fblocks = (s.N + kTileF - 1) / kTileF;
+    p.n_mblocks = (s.M + t.bm - 1) / t.bm;
+    p.split = t.split;
+    p.items = t.items;
+    p.x = x; p.w = w; p.ldx = s.ldx; p.ldw = s.ldw;
+    p.epi = epi;
+    p.status = status;
+    const int eb = s.type == MNN_TYPE_FP32 ? 4 : 2;
+    CUtensorMap mx = {}, mw = {};
+    if (!t.copy && (!encode_rows_map(&mx, x, eb, s.K, s.M, s.ldx, t.bm) || !encode_rows_map(&mw, w, eb, s.K, s.N, s.ldw, kTileF))) {
+        *why = "cuTensorMapEncodeTiled failed or is unavailable";
+        return cudaErrorInvalidValue;
+    }
+    // two blocks of K per stage where the loop is long enough (a wait and a commit cost the issuing thread more than the four
+    // instructions of a block) and that leaves three stages
+    const long long blocks = ((long long)s.K * eb + 127) / 128 / t.split;
+    const bool two = blocks >= 4 && t.bm <= 128;
+    switch (s.type) {
+        case MNN_TYPE_FP32: return run_type<MNN_TYPE_FP32, 1>(t, p, num_sms, mx, mw, stream);
+        case MNN_TYPE_BF16: return two ? run_type<MNN_TYPE_BF16, 2>(t, p, num_sms, mx, mw, stream) : run_type<MNN_TYPE_BF16, 1>(t, p, num_sms, mx, mw, stream);
+        default: return two ? run_type<MNN_TYPE_FP16, 2>(t, p, num_sms, mx, mw, stream) : run_type<MNN_TYPE_FP16, 1>(t, p, num_sms, mx, mw, stream);
+    }
+}
+
+}  // namespace mnnb

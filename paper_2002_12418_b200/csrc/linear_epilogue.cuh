@@ -1,0 +1,111 @@
+// What the kernels of the matrix product over rows share: element types, activations, and the order of work items.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "../../include/mnn_conv.h"
+#include "linear.h"
+
+namespace mnnb {
+
+template <int TYPE> struct Elem;
+template <> struct Elem<MNN_TYPE_FP32> {
+    typedef float T;
+    static __device__ __forceinline__ float load(const T* p) { return *p; }
+    static __device__ __forceinline__ T round(float v) { return v; }
+};
+template <> struct Elem<MNN_TYPE_BF16> {
+    typedef __nv_bfloat16 T;
+    static __device__ __forceinline__ float load(const T* p) { return __bfloat162float(*p); }
+    static __device__ __forceinline__ T round(float v) { return __float2bfloat16_rn(v); }
+};
+template <> struct Elem<MNN_TYPE_FP16> {
+    typedef __half T;
+    static __device__ __forceinline__ float load(const T* p) { return __half2float(*p); }
+    static __device__ __forceinline__ T round(float v) { return __float2half_rn(v); }
+};
+
+// v / (1 + e^-t): with the fast exponential and division where the result is rounded to 16 bits (their errors, a few parts in
+// 2^22, vanish in a rounding of 2^-9 or 2^-12), with the exact ones in fp32.
+template <int TYPE>
+__device__ __forceinline__ float times_logistic(float v, float t)
+{
+    return TYPE == MNN_TYPE_FP32 ? v / (1.0f + expf(-t)) : __fdividef(v, 1.0f + __expf(-t));
+}
+
+// The activations keep a NaN a NaN (ReLU too, unlike fmaxf).
+template <int TYPE, int NUM>
+__device__ __forceinline__ void activate(float (&v)[NUM], int act)
+{
+    if (act == MNN_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < NUM; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];
+    } else if (act == MNN_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < NUM; ++j) v[j] = 0.5f * v[j] * (1.0f + erff(v[j] * 0.70710678118654752f));
+    } else if (act == MNN_ACT_GELU_TANH) {
+        // (1 + tanh z) / 2 = 1 / (1 + e^-2z),  2 z = 2 sqrt(2/pi) (v + 0.044715 v^3)
+#pragma unroll
+        for (int j = 0; j < NUM; ++j) v[j] = times_logistic<TYPE>(v[j], 1.5957691216057308f * v[j] * fmaf(0.044715f * v[j], v[j], 1.0f));
+    } else if (act == MNN_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < NUM; ++j) v[j] = times_logistic<TYPE>(v[j], v[j]);
+    }
+}
+
+// Sums of NUM rows m0.. of x for one feature n -> y.  `rows` of them exist.  In a warp the lanes are 32 consecutive features,
+// so that every load of the residual and every store of y is one contiguous run of 32 elements, whatever the alignment.
+template <int TYPE, int NUM>
+struct LinearStore {
+    typedef typename Elem<TYPE>::T T;
+    typename Elem<TYPE>::T r[NUM];
+    __device__ __forceinline__ void fetch(const LinearEpilogue& e, long long m0, int rows, int n, bool n_ok)
+    {
+        if (e.res_mode == MNN_RESIDUAL_NONE || !n_ok) return;
+        const T* p = static_cast<const T*>(e.residual) + m0 * e.ldr + n;
+#pragma unroll
+        for (int j = 0; j < NUM; ++j)
+            if (j < rows) r[j] = p[j * e.ldr];
+    }
+    __device__ __forceinline__ void store(const LinearEpilogue& e, float (&v)[NUM], float bias, long long m0, int rows, int n, bool n_ok)
+    {
+        if (!n_ok) return;
+#pragma unroll
+        for (int j = 0; j < NUM; ++j) v[j] += bias;
+        if (e.res_mode == MNN_RESIDUAL_BEFORE) {
+#pragma unroll
+            for (int j = 0; j < NUM; ++j)
+                if (j < rows) v[j] += Elem<TYPE>::load(&r[j]);
+        }
+        activate<TYPE>(v, e.act);
+        if (e.res_mode == MNN_RESIDUAL_AFTER) {
+#pragma unroll
+            for (int j = 0; j < NUM; ++j)
+                if (j < rows) v[j] += Elem<TYPE>::load(&r[j]);
+        }
+        T* q = static_cast<T*>(e.y) + m0 * e.ldy + n;
+#pragma unroll
+        for (int j = 0; j < NUM; ++j)
+            if (j < rows) q[j * e.ldy] = Elem<TYPE>::round(v[j]);
+    }
+};
+
+template <int TYPE>
+__device__ __forceinline__ float linear_bias(const LinearEpilogue& e, int n, bool n_ok)
+{
+    return e.bias && n_ok ? Elem<TYPE>::load(static_cast<const typename Elem<TYPE>::T*>(e.bias) + n) : 0.0f;
+}
+
+// Work items in groups of eight feature blocks, the feature block running fastest within a group: the items that run at one time
+// cover a compact rectangle of the result, and their operands are read from L2 by several of them.
+__device__ __forceinline__ void linear_item(long long item, int n_fblocks, int n_mblocks, int* fb, int* mb)
+{
+    const long long per_group = 8ll * n_mblocks;
+    const int g = (int)(item / per_group);
+    const int rem = (int)(item - g * per_group);
+    const int width = min(8, n_fblocks - g * 8);
+    *mb = rem / width;
+    *fb = g * 8 + (rem - *mb * width);
+}
+
+}  // namespace mnnb

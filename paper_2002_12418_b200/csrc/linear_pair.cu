@@ -1,0 +1,271 @@
+// The matrix product over rows of linear.cu for many rows of 16-bit operands, on PAIRS of SMs: two CTAs of a cluster work on
+// 256 features x 256 rows of x per work item with tcgen05.mma.cta_group::2.  Each CTA stages its own 128 rows of w and HALF of
+// the x tile (128 of the 256 rows); the tensor cores of both SMs read both halves, and each CTA's tensor memory receives its own
+// 128 features x 256 rows.  A CTA therefore pulls 2 x 128 operand rows per block of K where a CTA on its own would pull
+// 128 + 256 for the same product: 64 bytes a clock at the tensor core's rate instead of 96, more than L2 delivers to an SM.
+//
+// Barriers as in contract_pair.cu: "operands landed" lives in the first CTA and counts the bytes of both CTAs' copies; "stage
+// free" and "accumulator complete" are signalled in both CTAs by one multicast commit; "accumulator drained" lives in the first
+// CTA and collects the epilogue warps of both.  No copy is multicast.  All waits are local and bounded; a CTA leaves only after
+// a cluster barrier, so that nothing is signalled into shared memory that is gone.
+#include "cluster.cuh"
+#include "linear_epilogue.cuh"
+#include "kernels.h"
+#include "umma.cuh"
+
+namespace mnnb {
+
+namespace {
+
+constexpr int kRows = 128;               // rows of w, and rows of x, per CTA and stage
+constexpr int kPairN = 256;              // rows of x per work item
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kStages = 6;
+constexpr uint32_t kTileBytes = kRows * 128, kStageBytes = 2 * kTileBytes;
+constexpr int kSmem = 200 * 1024;        // one CTA per SM
+constexpr int kErrProducer = 61, kErrMmaFull = 62, kErrMmaTmem = 63, kErrEpilogue = 64;   // status codes
+
+struct PairLinearParams {
+    int M, N, n_fblocks, n_mblocks, k_blocks;
+    long long items;
+    LinearEpilogue epi;
+    int* status;
+};
+
+__device__ __forceinline__ void remote_arrive(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// Tiled copy into THIS CTA's shared memory whose bytes are counted on a barrier given by its cluster address.
+__device__ __forceinline__ void pair_load_2d(uint32_t dst_smem, const CUtensorMap* map, uint32_t cluster_bar, int c0, int c1)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst_smem), "l"(reinterpret_cast<uint64_t>(map)), "r"(cluster_bar), "r"(c0), "r"(c1)
+        : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t accumulate)
+{
+    const uint32_t z = 0;
+    asm volatile(
+        "{\n\t.reg .b64 da, db;\n\t.reg .pred p;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, {%6, %6, %6, %6, %6, %6, %6, %6}, p;\n\t}" ::"r"(d_tmem), "r"(a_lo),
+        "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate), "r"(z)
+        : "memory");
+}
+// Arrive on the barrier at this shared-memory offset in both CTAs once the MMAs issued so far have completed.
+__device__ __forceinline__ void pair_commit(uint32_t bar)
+{
+    const unsigned short both = 3;
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(both)
+                 : "memory");
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, PairLinearParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full_bar[kStages];
+    __shared__ __align__(8) uint64_t empty_bar[kStages];
+    __shared__ __align__(8) uint64_t tfull_bar[2];
+    __shared__ __align__(8) uint64_t tempty_bar[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_ctarank();
+    const long long pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    volatile int* abortp = &abort_flag;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&full_bar[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&empty_bar[s]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&tfull_bar[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&tempty_bar[s]), 2 * kEpiWarps);
+        }
+        abort_flag = 0;
+        ptx::fence_barrier_init();
+        ptx::prefetch_tensormap(&map_x);
+        ptx::prefetch_tensormap(&map_w);
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::cluster_sync_all();                  // both CTAs' barriers exist before anything is signalled across
+    ptx::tc_fence_after();
+    const uint32_t tmem_base = tmem_slot;
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+    auto failed = [&](int code) {             // called by one lane
+        if (!*abortp) atomicCAS(p.status, 0, code);
+        *abortp = 1;
+    };
+
+    if (warp == 0) {
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        for (long long item = pair; item < p.items && ok; item += n_pairs) {
+            int fb, mb;
+            linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
+            const int w_row = (fb * 2 + (int)rank) * kRows, x_row = mb * kPairN + (int)rank * kRows;
+            for (int kb = 0; kb < p.k_blocks; ++kb) {
+                if (!ptx::mbar_wait_warp(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp)) {
+                    if (lane == 0) failed(kErrProducer);
+                    ok = false;
+                    break;
+                }
+                // the first CTA's barrier counts the bytes of both CTAs' copies
+                const uint32_t bar = ptx::map_to_rank(ptx::smem_u32(&full_bar[stage]), 0);
+                const uint32_t sbase = smem_base + stage * kStageBytes;
+                if (ptx::elect_one()) {
+                    if (rank == 0) ptx::mbar_expect_tx(ptx::smem_u32(&full_bar[stage]), 2u * kStageBytes);
+                    pair_load_2d(sbase, &map_w, bar, kb * 64, w_row);
+                    pair_load_2d(sbase + kTileBytes, &map_x, bar, kb * 64, x_row);
+                }
+                if (++stage == (uint32_t)kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0) {
+            const uint32_t idesc = ptx::mma_idesc(TYPE == MNN_TYPE_BF16 ? 1 : 0, 2 * kRows, kPairN);
+            constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            const uint32_t a_lo0 = ((smem_base & 0x3FFFFu) >> 4) | (1u << 16);
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            bool ok = true;
+            for (long long item = pair; item < p.items && ok; item += n_pairs) {
+                if (!ptx::mbar_wait_warp(ptx::smem_u32(&tempty_bar[acc]), acc_phase ^ 1u, abortp)) {
+                    if (lane == 0) failed(kErrMmaTmem);
+                    ok = false;
+                    break;
+                }
+                ptx::tc_fence_after();
+                const uint32_t d_tmem = tmem_base + acc * (uint32_t)kPairN;
+                for (int kb = 0; kb < p.k_blocks; ++kb) {
+                    if (!ptx::mbar_wait_warp(ptx::smem_u32(&full_bar[stage]), phase, abortp)) {
+                        if (lane == 0) failed(kErrMmaFull);
+                        ok = false;
+                        break;
+                    }
+                    ptx::tc_fence_after();
+                    const uint32_t a = a_lo0 + stage * (kStageBytes >> 4), b = a + (kTileBytes >> 4);
+                    if (ptx::elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks) pair_mma(d_tmem, a + ks * 2, b + ks * 2, kDescHi, idesc, (kb | ks) != 0 ? 1u : 0u);
+                        pair_commit(ptx::smem_u32(&empty_bar[stage]));         // the stage is free in both CTAs
+                    }
+                    if (++stage == (uint32_t)kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                if (ptx::elect_one()) pair_commit(ptx::smem_u32(&tfull_bar[acc]));               // accumulator complete, both CTAs
+                acc ^= 1u;
+                if (acc == 0) acc_phase ^= 1u;
+            }
+        }
+    } else {
+        const int q = warp & 3;                       // tensor-memory lane quarter this warp may read
+        const int ch0 = ((warp - 2) >> 2) * 8, ch1 = ch0 + 8;       // its half of the 16 chunks of 16 rows
+        uint32_t acc = 0, acc_phase = 0;
+        for (long long item = pair; item < p.items; item += n_pairs) {
+            int fb, mb;
+            linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
+            const int n = (fb * 2 + (int)rank) * kRows + q * 32 + lane;
+            const bool n_ok = n < p.N;
+            const long long m_item = (long long)mb * kPairN;
+            const float bias = linear_bias<TYPE>(p.epi, n, n_ok);
+            LinearStore<TYPE, 16> out;
+            auto rows_at = [&](int ch) { return (int)min(16ll, p.M - (m_item + ch * 16)); };
+            out.fetch(p.epi, m_item + ch0 * 16, rows_at(ch0), n, n_ok);
+            int got = 1;
+            if (lane == 0) got = ptx::mbar_wait_relaxed(ptx::smem_u32(&tfull_bar[acc]), acc_phase, abortp) ? 1 : 0;
+            got = __shfl_sync(0xffffffffu, got, 0);
+            if (!got) {
+                if (lane == 0) failed(kErrEpilogue);
+                break;
+            }
+            ptx::tc_fence_after();
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * (uint32_t)kPairN;
+            uint32_t v[16];
+            ptx::tmem_ld16(taddr + (uint32_t)(ch0 * 16), v);
+            for (int ch = ch0; ch < ch1; ++ch) {
+                ptx::tmem_ld_wait();
+                float s[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[j] = __uint_as_float(v[j]);
+                LinearStore<TYPE, 16> now = out;
+                if (ch + 1 < ch1) {
+                    ptx::tmem_ld16(taddr + (uint32_t)((ch + 1) * 16), v);
+                    out.fetch(p.epi, m_item + (ch + 1) * 16, rows_at(ch + 1), n, n_ok);
+                }
+                now.store(p.epi, s, bias, m_item + ch * 16, rows_at(ch), n, n_ok);
+            }
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) remote_arrive(ptx::map_to_rank(ptx::smem_u32(&tempty_bar[acc]), 0));
+            acc ^= 1u;
+            if (acc == 0) acc_phase ^= 1u;
+        }
+    }
+
+    // Teardown.  After an aborted run give copies still in flight time to land; nobody leaves before both CTAs are here.
+    __syncwarp();
+    if (*abortp) __nanosleep(200000);
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::cluster_sync_all();
+    if (warp == 1) {
+        __syncwarp();
+        ptx::tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+template <int TYPE>
+cudaError_t run_pair(const PairLinearParams& p, int num_sms, const CUtensorMap& mx, const CUtensorMap& mw, cudaStream_t stream)
+{
+    static unsigned long long done = 0;
+    auto kern = linear_pair_kernel<TYPE>;
+    cudaError_t e = allow_smem_once(reinterpret_cast<const void*>(kern), kSmem, &done);
+    if (e != cudaSuccess) return e;
+    const long long max_pairs = num_sms / 2, pairs = p.items < max_pairs ? p.items : max_pairs;
+    return launch_cluster(2, kern, dim3((unsigned)(2 * pairs)), dim3(kThreads), (size_t)kSmem, stream, mx, mw, p);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_pair(const LinearShape& s, const LinearTiling& t, int num_sms, const void* x, const void* w,
+                               const LinearEpilogue& epi, int* status, cudaStream_t stream, const char** why)
+{
+    PairLinearParams p = {};
+    p.M = s.M; p.N = s.N;
+    p.n_fblocks = (s.N + 2 * kRows - 1) / (2 * kRows);
+    p.n_mblocks = (s.M + kPairN - 1) / kPairN;
+    p.k_blocks = (s.K + 63) / 64;
+    p.items = t.items;
+    p.epi = epi;
+    p.status = status;
+    CUtensorMap mx, mw;
+    if (!encode_rows_map(&mx, x, 2, s.K, s.M, s.ldx, kRows) || !encode_rows_map(&mw, w, 2, s.K, s.N, s.ldw, kRows)) {
+        *why = "cuTensorMapEncodeTiled failed or is unavailable";
+        return cudaErrorInvalidValue;
+    }
+    return s.type == MNN_TYPE_BF16 ? run_pair<MNN_TYPE_BF16>(p, num_sms, mx, mw, stream) : run_pair<MNN_TYPE_FP16>(p, num_sms, mx, mw, stream);
+}
+
+}  // namespace mnnb

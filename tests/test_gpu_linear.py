@@ -1,0 +1,218 @@
+"""GPU parity of the matrix product over rows (mnn_linear_*) against its definition in fp64.
+
+Tolerance, per element, with S = the sum of the absolute terms (products, bias, residual):
+* products of 16-bit values are exact in fp32; the tensor core adds 16 of them per step and cuts the sum off, at most 2^-23 of
+  the running sum, which never exceeds S: (K / 16 + 8) 2^-23 S, the 8 for the joins of a cluster, bias and residual;
+* fp32 operands lose at most 2^-20 each to the cut of their low halves and 2^-20 to the product of the low halves (both halves
+  are cut off, not rounded: |lo| < 2^-10 |v|): 3 * 2^-20 S; 16 steps of 8 per segment of 128 elements, cut off: 16 * 2^-23 S, one
+  rounded addition per segment: (K / 128 + 8) 2^-24 S;
+* the activations have slopes of at most 1.13; their own evaluation errs by at most 2^-19 of the value with the fast
+  exponential and division (16-bit types), 2^-21 of the value with the exact ones;
+* one rounding at the store: half an eps of the type.
+"""
+import numpy as np
+import pytest
+
+from oracle import rows as oracle
+from paper_2002_12418_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+HALF_EPS = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+
+
+def bound(y, s, size, K, dtype):
+    if dtype == "fp32":
+        err = (3 * 2.0 ** -20 + 16 * 2.0 ** -23 + (K / 128 + 8) * 2.0 ** -24) * size
+        own = 2.0 ** -21
+    else:
+        err = (K / 16 + 8) * 2.0 ** -23 * size
+        own = 2.0 ** -19
+    err = 1.13 * err + own * np.abs(s) + 1e-30
+    tiny = 2.0 ** -25 if dtype == "fp16" else 0.0          # half the spacing of the smallest halves
+    return err + HALF_EPS[dtype] * (np.abs(y) + err) + tiny
+
+
+def make(torch, seed, shape, ld, dtype, scale=1.0, offset=0):
+    """Rows `ld` elements apart, `offset` elements behind an aligned address; what lies between rows is NaN."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    flat = torch.full((offset + shape[0] * ld + 16,), float("nan"), dtype=t, device="cuda")
+    view = flat[offset:offset + shape[0] * ld].view(shape[0], ld)[:, :shape[1]]
+    view.copy_(torch.randn(shape, generator=g, device="cuda") * scale)
+    return view
+
+
+def host(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def run_case(M, K, N, dtype, act="none", mode="none", bias=True, pads=(0, 0, 0, 0), offset=0, seed=0, in_place=False):
+    import torch
+    ldx, ldw, ldy, ldr = K + pads[0], K + pads[1], N + pads[2], N + pads[3]
+    x = make(torch, seed, (M, K), ldx, dtype, offset=offset)
+    w = make(torch, seed + 1, (N, K), ldw, dtype, K ** -0.5, offset=offset)
+    b = make(torch, seed + 2, (1, N), N, dtype, 0.5)[0].contiguous() if bias else None
+    r = make(torch, seed + 3, (M, N), ldr, dtype) if mode != "none" else None
+    runner = B.LinearRunner(M, N, K, dtype, act, mode, ldx, ldw, ldy, ldr)
+    want, s, size = oracle.linear(host(x), host(w), host(b), host(r), act, mode)
+    if in_place:
+        y = r
+    else:
+        whole = torch.full((M, ldy), 7.0, dtype=x.dtype, device="cuda")
+        y = whole[:, :N]
+    runner.run(x, w, b, r, y)
+    torch.cuda.synchronize()
+    assert runner.device_status() == 0
+    got = host(y)
+    over = np.abs(got - want) - bound(want, s, size, K, dtype)
+    assert np.isfinite(got).all() and (over <= 0).all(), "worst excess %.3e at %s" % (over.max(), np.unravel_index(over.argmax(), over.shape))
+    if not in_place and ldy > N:
+        assert (whole[:, N:] == 7.0).all(), "columns behind the rows' end were written"
+    info = runner.info
+    runner.close()
+    return got, info
+
+
+# every type; a single row, a few, and sizes around the tiles of 16..256 rows, 128 features and 32 or 64 elements of K
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (1, 64, 128), (1, 1024, 1000), (3, 72, 130), (16, 512, 640), (17, 96, 256), (33, 200, 129),
+                                   (64, 2048, 512), (100, 328, 385), (129, 640, 127), (257, 256, 300), (700, 136, 1000)])
+def test_sizes(M, K, N, dtype):
+    run_case(M, K, N, dtype, seed=M + K + N)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("mode", ["none", "after", "before"])
+def test_epilogues(act, mode, dtype):
+    run_case(37, 264, 200, dtype, act, mode, seed=5)
+    run_case(300, 264, 1040, dtype, act, mode, bias=False, seed=6)
+
+
+# rows that TMA cannot copy: odd lengths and strides, odd base addresses
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("M,K,N,pads,offset", [(1, 7, 5, (0, 0, 0, 0), 0), (5, 1001, 131, (0, 0, 0, 0), 1), (77, 1001, 513, (3, 0, 3, 3), 0),
+                                               (40, 64, 96, (1, 8, 0, 0), 0), (130, 333, 260, (2, 5, 1, 7), 3), (16, 4096, 300, (0, 0, 0, 0), 1),
+                                               (600, 129, 700, (0, 0, 0, 0), 0)])
+def test_unaligned_rows(M, K, N, pads, offset, dtype):
+    run_case(M, K, N, dtype, "silu", "after", pads=pads, offset=offset, seed=M + K)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_padded_rows_by_tma(dtype):
+    _, info = run_case(70, 128, 200, dtype, "relu", "before", pads=(8, 16, 1, 24), seed=9)
+    assert not info.copy
+
+
+def test_residual_in_place():
+    run_case(50, 256, 300, "bf16", "none", "after", seed=11, in_place=True)
+    run_case(520, 256, 2048, "fp32", "relu", "before", seed=12, in_place=True)
+
+
+# the kernel on pairs of SMs, at sizes off its 256 x 256 blocks
+@pytest.mark.parametrize("dtype,M,K,N", [("bf16", 2048, 512, 4096), ("fp16", 1900, 520, 4200), ("bf16", 4001, 72, 3001 // 8 * 8 + 3)])
+def test_pairs(dtype, M, K, N):
+    _, info = run_case(M, K, N, dtype, "silu", "after", seed=21)
+    assert info.pair
+
+
+# integers small enough that every sum is exact: any correct evaluation is bit-identical
+@pytest.mark.parametrize("dtype,M,K,N", [("fp32", 200, 300, 260), ("bf16", 200, 296, 260), ("fp16", 200, 299, 260), ("bf16", 2048, 256, 4096),
+                                         ("fp32", 4, 4096, 256), ("bf16", 4, 4096, 256)])
+def test_integers_are_exact(dtype, M, K, N):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    x = torch.randint(-4, 5, (M, K), generator=g, device="cuda").to(t)
+    w = torch.randint(-4, 5, (N, K), generator=g, device="cuda").to(t)
+    b = torch.randint(-4, 5, (N,), generator=g, device="cuda").to(t)
+    r = B.LinearRunner(M, N, K, dtype)
+    y = r.run(x, w, b)
+    want = (x.double() @ w.double().t() + b.double()).to(t)
+    assert torch.equal(y, want) and r.device_status() == 0
+    y2 = r.run(x, w, b)
+    assert torch.equal(y, y2)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("K", [96, 101, 2048])
+def test_infinities_and_nan(dtype, K):
+    import torch
+    M, N = 20, 140
+    x = make(torch, 1, (M, K), K, dtype)
+    w = make(torch, 2, (N, K), K, dtype)
+    x[3, 5], x[4, K - 1], x[6, 2], w[7, 9] = float("inf"), float("-inf"), float("nan"), float("inf")
+    w[9, 5] = 0.0                                    # infinity times zero
+    r = B.LinearRunner(M, N, K, dtype)
+    got = host(r.run(x, w))
+    want, s, size = oracle.linear(host(x), host(w))
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want))
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    fine = np.isfinite(want)
+    assert (np.abs(got - want)[fine] <= bound(want, s, size, K, dtype)[fine]).all()
+    assert r.device_status() == 0
+
+
+def test_relu_keeps_nan_and_half_overflows_to_infinity():
+    import torch
+    x = torch.full((2, 64), 200.0, dtype=torch.float16, device="cuda")
+    w = torch.full((3, 64), 200.0, dtype=torch.float16, device="cuda")
+    x[1, 0] = float("nan")
+    y = B.LinearRunner(2, 3, 64, "fp16", act="relu").run(x, w)
+    assert torch.isinf(y[0]).all() and torch.isnan(y[1]).all()
+
+
+def test_graph_replay_other_stream_and_two_plans_at_once():
+    import torch
+    M, K, N = 24, 512, 1024
+    x, w = make(torch, 1, (M, K), K, "bf16"), make(torch, 2, (N, K), K, "bf16")
+    r, r2 = B.LinearRunner(M, N, K, "bf16", act="gelu"), B.LinearRunner(M, N, K, "bf16", act="gelu")
+    want = r.run(x, w)
+    y = torch.empty_like(want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        r.run(x, w, y=y)
+    y.zero_()
+    x2 = x.clone()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+    x.mul_(2)                                        # a replay reads what lies there now
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, r2.run(x, w)) and not torch.equal(y, want)
+    with torch.cuda.stream(side):
+        a = r.run(x2, w)
+    b = r2.run(x2, w)
+    torch.cuda.synchronize()
+    assert torch.equal(a, want) and torch.equal(b, want)
+
+
+def test_refusals_of_tensors():
+    import torch
+    r = B.LinearRunner(4, 8, 16, "bf16", residual="after")
+    x, w, y = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((4, 16), (8, 16), (4, 8)))
+    res = torch.zeros_like(y)
+    r.run(x, w, None, res, y)
+    for bad in (dict(x=x.float()), dict(x=x[:3]), dict(x=x.cpu()), dict(w=w.t()), dict(residual=None), dict(bias=torch.zeros(7, device="cuda", dtype=torch.bfloat16)),
+                dict(y=torch.zeros(4, 9, dtype=torch.bfloat16, device="cuda")[:, :8])):
+        a = dict(x=x, w=w, bias=None, residual=res, y=y)
+        a.update(bad)
+        with pytest.raises(B.MnnError) as e:
+            r.run(a["x"], a["w"], a["bias"], a["residual"], a["y"])
+        assert e.value.code == B.MNN_EINVAL
+    # overlapping memory: y inside x; y one row behind its residual
+    flat = torch.zeros(16 * 16, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(B.MnnError):
+        r.run(flat[:64].view(4, 16), w, None, res, flat[8:40].view(4, 8))
+    with pytest.raises(B.MnnError):
+        r.run(x, w, None, flat[:32].view(4, 8), flat[8:40].view(4, 8))
+    # columns side by side in one buffer do not overlap
+    both = torch.zeros(4, 24, dtype=torch.bfloat16, device="cuda")
+    B.LinearRunner(4, 8, 16, "bf16", ldx=24, ldy=24).run(both[:, :16], w, y=both[:, 16:])
+    torch.cuda.synchronize()

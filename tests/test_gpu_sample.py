@@ -1,0 +1,219 @@
+"""GPU parity of sampling (mnn_sample_*) against its definition in fp64, row by row.  Tokens have to be equal; a probability is
+a quotient of two fp64 figures rounded once to fp32, where the mass in the denominator is a sum of weights rounded to 2^-43 or
+finer each: 2^-23 relative covers both, and 1e-37 what fp32 cannot hold."""
+import numpy as np
+import pytest
+
+from oracle import rows as oracle
+from paper_2002_12418_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def types(torch):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def check(logits, u, probs=True, runner=None, **given):
+    import torch
+    rows, vocab = logits.shape
+    name = {v: k for k, v in types(torch).items()}[logits.dtype]
+    r = runner or B.SampleRunner(rows, vocab, name, ld=logits.stride(0) if rows > 1 else 0)
+    token, prob, dist = r.run(logits, u, probs=probs, **given)
+    token2, prob2, _ = r.run(logits, u, probs=probs, **given)
+    torch.cuda.synchronize()
+    assert torch.equal(token, token2) and torch.equal(prob, prob2)
+    token, prob = token.cpu().numpy(), prob.double().cpu().numpy()
+    dist = dist.double().cpu().numpy() if dist is not None else None
+    l = logits.double().cpu().numpy()
+    par = {k: v.double().cpu().numpy() for k, v in given.items() if v is not None}
+    uu = u.double().cpu().numpy()
+    for i in range(rows):
+        a = {k: (int(v[i]) if k == "top_k" else v[i]) for k, v in par.items()}
+        t, pr, ps = oracle.sample_row(l[i], uu[i], **a)
+        assert token[i] == t, "row %d: token %d, wanted %d (%s, u = %r)" % (i, token[i], t, a, uu[i])
+        assert abs(prob[i] - pr) <= 2.0 ** -23 * pr + 1e-37
+        if dist is not None:
+            assert (np.abs(dist[i] - ps) <= 2.0 ** -23 * ps + 1e-37).all()
+    return token
+
+
+def make(torch, seed, rows, vocab, dtype, pad=0, scale=2.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    l = torch.randn(rows, vocab + pad, generator=g, device="cuda") * scale
+    return l.to(types(torch)[dtype])[:, :vocab], torch.rand(rows, generator=g, device="cuda"), g
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,vocab,pad", [(1, 1, 0), (3, 2, 1), (5, 33, 0), (1, 1000, 0), (40, 1001, 3), (9, 4099, 0), (4, 32000, 0), (2, 100003, 1), (1, 131072, 0)])
+def test_sizes(rows, vocab, pad, dtype):
+    import torch
+    l, u, g = make(torch, rows + vocab, rows, vocab, dtype, pad)
+    t = torch.rand(rows, generator=g, device="cuda") + 0.3
+    k = torch.randint(1, max(2, min(vocab, 300)), (rows,), generator=g, device="cuda", dtype=torch.int32)
+    p = torch.rand(rows, generator=g, device="cuda") * 0.5 + 0.5
+    q = torch.rand(rows, generator=g, device="cuda") * 0.1
+    check(l, u)
+    check(l, u, temperature=t)
+    check(l, u, temperature=t, top_k=k)
+    check(l, u, temperature=t, top_p=p)
+    check(l, u, temperature=t, min_p=q)
+    check(l, u, temperature=t, top_k=k, top_p=p, min_p=q)
+    check(l, u, probs=False, temperature=t, top_p=p, min_p=q)
+
+
+def test_largest_vocabulary():
+    import torch
+    for dtype in ("fp32", "bf16"):
+        l, u, g = make(torch, 5, 2, B.SAMPLE_MAX_VOCAB, dtype, 1)
+        check(l, u, top_p=torch.tensor([0.9, 0.5], device="cuda"), top_k=torch.tensor([100000, 0], device="cuda", dtype=torch.int32))
+
+
+def test_many_rows():
+    import torch
+    l, u, g = make(torch, 6, 700, 257, "fp32")
+    check(l, u, top_p=torch.rand(700, generator=g, device="cuda"))
+
+
+# masks: rows half hidden, rows with one candidate, rows with none; the lowest value of the type instead of -infinity
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [50, 9000])
+def test_masks(vocab, dtype):
+    import torch
+    l, u, g = make(torch, 8, 12, vocab, dtype)
+    low = torch.finfo(l.dtype).min
+    l[0] = float("-inf")
+    l[1] = float("nan")
+    l[2] = low
+    l[3, 1:] = float("-inf")
+    l[4, :-1] = low
+    l[5, torch.rand(vocab, generator=g, device="cuda") < 0.7] = float("-inf")
+    l[6, torch.rand(vocab, generator=g, device="cuda") < 0.7] = float("nan")
+    l[7, torch.rand(vocab, generator=g, device="cuda") < 0.7] = low
+    l[8, 3], l[8, 40] = float("inf"), float("inf")
+    l[9] = 0.0
+    l[10] = torch.where(torch.rand(vocab, generator=g, device="cuda") < 0.5, 0.0, -0.0).to(l.dtype)
+    l[11, 7] = torch.finfo(l.dtype).max
+    k = torch.full((12,), 20, dtype=torch.int32, device="cuda")
+    p = torch.full((12,), 0.8, device="cuda")
+    for given in ({}, dict(top_k=k), dict(top_p=p), dict(top_k=k, top_p=p), dict(min_p=p), dict(temperature=p * 0), dict(temperature=p / 0),
+                  dict(temperature=p / 0, top_k=k, top_p=p)):
+        token = check(l, u, **given)
+        assert token[0] == -1 and token[1] == -1 and token[3] == 0
+
+
+# values that tie by the thousand: the first ones by index stay
+@pytest.mark.parametrize("vocab", [100, 20011])
+@pytest.mark.parametrize("levels", [1, 2, 5])
+def test_ties(vocab, levels):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(levels)
+    rows = 16
+    l = torch.randint(0, levels, (rows, vocab), generator=g, device="cuda").to(torch.bfloat16)
+    u = torch.rand(rows, generator=g, device="cuda")
+    k = torch.randint(1, vocab + 2, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    p = torch.rand(rows, generator=g, device="cuda")
+    check(l, u, top_k=k)
+    check(l, u, top_p=p)
+    check(l, u, top_k=k, top_p=p)
+    check(l, u, temperature=torch.zeros(rows, device="cuda"))
+
+
+# parameters at and beyond their ends
+def test_edges_of_the_parameters():
+    import torch
+    nan, inf = float("nan"), float("inf")
+    l, _, _ = make(torch, 9, 12, 700, "fp32")
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 2.0, -1.0, nan, 0.5, 0.5, 0.5, 0.5, 0.5, 0.5], device="cuda")
+    t = torch.tensor([1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 0.0, -1.0, nan, 1e-30, 1e30, inf], device="cuda")
+    check(l, u, temperature=t)
+    k = torch.tensor([0, -5, 1, 2, 699, 700, 701, 2 ** 31 - 1, 3, 3, 3, 3], device="cuda", dtype=torch.int32)
+    check(l, u, top_k=k)
+    p = torch.tensor([0.0, -1.0, 1.0, 2.0, 1e-30, 1.0 - 2.0 ** -24, 0.5, nan, 0.3, 0.3, 0.3, 0.3], device="cuda")
+    check(l, u, top_p=p)
+    q = torch.tensor([0.0, -1.0, 1.0, 2.0, 1e-30, 1.0 - 2.0 ** -24, 0.5, 0.1, 0.3, 0.3, 0.3, 0.3], device="cuda")
+    check(l, u, min_p=q)
+    check(l, u, temperature=t, top_k=k, top_p=p, min_p=q)
+
+
+def test_wide_and_narrow_rows():
+    import torch
+    for scale in (1e-6, 1e-3, 30.0, 1e4, 1e30):
+        l, u, g = make(torch, 10, 8, 5000, "fp32", scale=scale)
+        p = torch.rand(8, generator=g, device="cuda")
+        k = torch.randint(1, 3000, (8,), generator=g, device="cuda", dtype=torch.int32)
+        check(l, u, top_p=p)
+        check(l, u, top_k=k, top_p=p)
+
+
+# the draws follow the distribution: 20000 equal rows, the frequency of each token within 6 standard deviations
+def test_draws_follow_the_distribution():
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    n = 20000
+    l = torch.tensor([0.0, 1.0, 2.0, float("-inf"), 0.5, -1.0, 2.0, -3.0], device="cuda").repeat(n, 1)
+    token, _, dist = B.SampleRunner(n, 8).run(l, torch.rand(n, generator=g, device="cuda"), probs=True)
+    p = dist[0].double().cpu().numpy()
+    seen = np.bincount(token.cpu().numpy(), minlength=8) / n
+    assert (np.abs(seen - p) <= 6 * np.sqrt(p * (1 - p) / n) + 1e-12).all()
+
+
+def test_what_lies_around_is_left_alone_and_graphs_replay():
+    import torch
+    l, u, g = make(torch, 11, 6, 999, "bf16", 1)
+    r = B.SampleRunner(6, 999, "bf16", ld=1000)
+    before = l.clone()
+    token = torch.full((8,), 77, dtype=torch.int32, device="cuda")
+    prob = torch.full((8,), 7.0, device="cuda")
+    whole = torch.full((7 * 999,), 7.0, device="cuda")
+    r.run(l, u, token=token[1:7], prob=prob[1:7], probs=whole[:6 * 999].view(6, 999))
+    torch.cuda.synchronize()
+    assert token[0] == 77 and token[7] == 77 and prob[0] == 7.0 and prob[7] == 7.0 and (whole[6 * 999:] == 7.0).all()
+    assert torch.equal(l, before)
+    want = token[1:7].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    out, pr = torch.empty_like(want), torch.empty(6, device="cuda")
+    with torch.cuda.graph(graph, stream=side):
+        r.run(l, u, token=out, prob=pr)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    u.fill_(0.999)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, r.run(l, u)[0])
+
+
+def test_refusals_of_tensors():
+    import torch
+    r = B.SampleRunner(4, 100, "bf16")
+    l, u = torch.zeros(4, 100, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, device="cuda")
+    r.run(l, u)
+    for a in ((l.float(), u), (l[:3], u), (l, u.double()), (l, u[:3]), (l, None), (l.cpu(), u)):
+        with pytest.raises(B.MnnError) as e:
+            r.run(*a)
+        assert e.value.code == B.MNN_EINVAL
+    with pytest.raises(B.MnnError):
+        r.run(l, u, top_k=torch.zeros(4, device="cuda"))
+    with pytest.raises(B.MnnError):
+        r.run(l, u, probs=torch.zeros(4, 100, device="cuda", dtype=torch.float64))
+    torch.cuda.synchronize()
+
+
+# the run of both: logits from the product, a token from the logits
+def test_logits_and_draw_together():
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    for dtype, M, K, V in (("bf16", 5, 256, 5003), ("fp32", 3, 128, 1000), ("fp16", 33, 264, 2048)):
+        t = types(torch)[dtype]
+        h = torch.randn(M, K, generator=g, device="cuda").to(t)
+        table = torch.randn(V, K, generator=g, device="cuda").mul_(0.3).to(t)
+        logits = B.LinearRunner(M, V, K, dtype).run(h, table)
+        check(logits, torch.rand(M, generator=g, device="cuda"), top_p=torch.full((M,), 0.9, device="cuda"))

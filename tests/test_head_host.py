@@ -1,0 +1,134 @@
+"""Host-side checks of the matrix product over rows and of sampling: arguments that are refused, what a plan decides, and the
+oracle on cases worked by hand.  No GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import rows as oracle
+from paper_2002_12418_b200 import binding as B
+
+
+def linear(*a, **kw):
+    p = B.mnn_linear_plan(*a, B.make_linear_opts(**kw))
+    info = B.mnn_linear_plan_query(p)
+    B.mnn_linear_destroy(p)
+    return info
+
+
+def test_struct_layouts_match_the_header():
+    assert ctypes.sizeof(B.LinearOpts) == 4 * 4 + 4 * 8 and ctypes.sizeof(B.LinearInfo) == 10 * 4 + 2 * 8
+    assert ctypes.sizeof(B.SampleOpts) == 2 * 4 + 2 * 8 and ctypes.sizeof(B.SampleInfo) == 6 * 4
+
+
+@pytest.mark.parametrize("shape", [(0, 1, 1), (1, 0, 1), (1, 1, 0), (-1, 4, 4), (4, -1, 4), (4, 4, -1)])
+def test_linear_refuses_sizes(shape):
+    with pytest.raises(B.MnnError):
+        linear(*shape)
+
+
+@pytest.mark.parametrize("kw", [dict(ldx=15), dict(ldw=15), dict(ldy=7), dict(ldr=7), dict(ldx=-16), dict(ldx=1 << 40), dict(dtype="fp64"),
+                                dict(act="tanh"), dict(residual="inside")])
+def test_linear_refuses_options(kw):
+    with pytest.raises(B.MnnError):
+        linear(4, 8, 16, **kw)
+
+
+def test_linear_refuses_values_outside_the_enumerations():
+    for field, value in (("type", 3), ("type", -1), ("act", 5), ("act", -1), ("residual", 3), ("residual", -1)):
+        o = B.make_linear_opts()
+        setattr(o, field, value)
+        with pytest.raises(B.MnnError):
+            B.mnn_linear_plan(4, 8, 16, o)
+
+
+def test_linear_refuses_runs():
+    p = B.mnn_linear_plan(4, 8, 16, B.make_linear_opts("bf16"))
+    q = B.mnn_linear_plan(4, 8, 16, B.make_linear_opts("bf16", residual="after"))
+    a, w, y = 1 << 20, 2 << 20, 3 << 20                   # addresses; nothing is launched
+    for code, call in ((B.MNN_EINVAL, lambda: B.mnn_linear_run(p, None, w, None, None, y, 0)),
+                       (B.MNN_EINVAL, lambda: B.mnn_linear_run(p, a, w, None, y, y, 0)),
+                       (B.MNN_EINVAL, lambda: B.mnn_linear_run(q, a, w, None, None, y, 0)),
+                       (B.MNN_EWORKSPACE, lambda: B.mnn_linear_run(p, a, w, None, None, y, 0)),
+                       (B.MNN_EWORKSPACE, lambda: B.mnn_linear_set_workspace(p, None, 4096)),
+                       (B.MNN_EWORKSPACE, lambda: B.mnn_linear_set_workspace(p, 1 << 20, 64)),
+                       (B.MNN_EALIGN, lambda: B.mnn_linear_set_workspace(p, (1 << 20) + 16, 4096))):
+        with pytest.raises(B.MnnError) as e:
+            call()
+        assert e.value.code == code, str(e.value)
+    B.mnn_linear_destroy(p)
+    B.mnn_linear_destroy(q)
+
+
+def test_linear_plans():
+    one = linear(1, 4096, 4096, dtype="bf16")
+    assert one.rows_per_item == 16 and one.split > 1 and not one.copy and not one.pair and one.workspace_bytes == 1024
+    assert linear(8192, 8192, 4096, dtype="bf16").pair and not linear(8192, 8192, 4096, dtype="fp32").pair
+    assert linear(64, 64, 1001, dtype="bf16").copy and linear(64, 64, 1001, dtype="bf16", ldx=1008, ldw=1008).copy == 0
+    assert linear(64, 64, 1002, dtype="fp32").copy
+    for M in (1, 2, 16, 17, 100, 1000):
+        for N in (1, 128, 1000, 50000):
+            for dtype in B.TYPES:
+                i = linear(M, N, 512, dtype=dtype)
+                per = 256 if i.pair else 128
+                assert i.items == -(-N // per) * -(-M // i.rows_per_item) and i.rows_per_item <= (128 if dtype == "fp32" else 256)
+                assert i.split in (1, 2, 4, 8)
+
+
+def test_sample_refusals():
+    for shape, kw in (((0, 5), {}), ((5, 0), {}), ((2, 10), dict(ld=9)), ((2, 10), dict(ld_probs=9)), ((2, B.SAMPLE_MAX_VOCAB + 1), {}),
+                      ((1 << 28, 10), {}), ((2, 10), dict(dtype="fp64")), ((2, 10), dict(ld=1 << 40))):
+        with pytest.raises(B.MnnError):
+            B.mnn_sample_plan(*shape, B.make_sample_opts(**kw))
+    p = B.mnn_sample_plan(2, 10, B.make_sample_opts("bf16"))
+    a = 1 << 20
+    for args in ((None, a, None, None, None, None, a, None, None), (a, None, None, None, None, None, a, None, None), (a, a, None, None, None, None, None, None, None)):
+        with pytest.raises(B.MnnError) as e:
+            B.mnn_sample_run(p, *args, 0)
+        assert e.value.code == B.MNN_EINVAL
+    for args in ((a + 1, a, None, None, None, None, a, None, None), (a, a + 2, None, None, None, None, a, None, None), (a, a, None, a + 1, None, None, a, None, None)):
+        with pytest.raises(B.MnnError) as e:
+            B.mnn_sample_run(p, *args, 0)
+        assert e.value.code == B.MNN_EALIGN
+    B.mnn_sample_destroy(p)
+
+
+def test_sample_plans_hold_their_rows():
+    for vocab in (1, 7, 1000, 32000, 131072, B.SAMPLE_MAX_VOCAB):
+        for rows in (1, 64, 1000):
+            for dtype in B.TYPES:
+                p = B.mnn_sample_plan(rows, vocab, B.make_sample_opts(dtype))
+                i = B.mnn_sample_plan_query(p)
+                B.mnn_sample_destroy(p)
+                assert i.ctas_per_row in (1, 2, 4, 8) and i.threads in (128, 256, 512)
+                assert vocab << i.scale_log2 <= 1 << 62            # the mass of a row of equal logits fits a 64-bit integer
+
+
+def test_oracle_by_hand():
+    l = np.log([0.1, 0.4, 0.2, 0.3])
+    # index order 0.1 | 0.5 | 0.7 | 1.0
+    assert [oracle.sample_row(l, u)[0] for u in (0.05, 0.11, 0.49, 0.51, 0.69, 0.71, 0.999)] == [0, 1, 1, 2, 2, 3, 3]
+    assert abs(oracle.sample_row(l, 0.2)[1] - 0.4) < 1e-12
+    # the two largest: indexes 1 (0.4) and 3 (0.3)
+    assert [oracle.sample_row(l, u, top_k=2)[0] for u in (0.0, 0.57, 0.58, 0.99)] == [1, 1, 3, 3]
+    # 0.4 + 0.3 reach 0.6; 0.4 alone does not
+    assert np.allclose(oracle.sample_row(l, 0.0, top_p=0.6)[2], [0, 4 / 7, 0, 3 / 7])
+    assert np.allclose(oracle.sample_row(l, 0.0, top_p=0.39)[2], [0, 1, 0, 0])
+    # of the three largest (mass 0.9), 0.4 and 0.3 lie before 0.8 of it (0.72)... and 0.7 < 0.72 keeps the third
+    assert np.allclose(oracle.sample_row(l, 0.0, top_k=3, top_p=0.8)[2], np.array([0, 4, 2, 3]) / 9)
+    assert np.allclose(oracle.sample_row(l, 0.0, min_p=0.6)[2], [0, 4 / 7, 0, 3 / 7])
+    # temperature 1/2 squares the weights
+    assert np.allclose(oracle.sample_row(l, 0.0, temperature=0.5)[2], np.array([1, 16, 4, 9]) / 30)
+    # equals: the lower index first
+    assert oracle.sample_row([1.0, 3.0, 3.0, 3.0], 0.9, top_k=2)[0] == 2 and oracle.sample_row([1.0, 3.0, 3.0], 0.9, temperature=0.0)[0] == 1
+    assert oracle.sample_row([-np.inf, np.nan], 0.5)[0] == -1
+
+
+def test_oracle_linear_by_hand():
+    y, s, size = oracle.linear([[1.0, -2.0]], [[3.0, 1.0], [0.5, 1.0]], [1.0, 0.0], np.array([[10.0, 1.0]]), "relu", "before")
+    assert s.tolist() == [[12.0, -0.5]] and y.tolist() == [[12.0, 0.0]] and size.tolist() == [[16.0, 3.5]]
+    y, _, _ = oracle.linear([[1.0, -2.0]], [[3.0, 1.0], [0.5, 1.0]], [1.0, 0.0], np.array([[10.0, 1.0]]), "relu", "after")
+    assert y.tolist() == [[12.0, 1.0]]
+    assert abs(oracle.activate(np.array(1.0), "gelu") - 0.8413447460685429) < 1e-15
+    assert abs(oracle.activate(np.array(1.0), "gelu_tanh") - 0.8411919906082768) < 1e-15
+    assert abs(oracle.activate(np.array(1.0), "silu") - 0.7310585786300049) < 1e-15
