@@ -474,7 +474,7 @@ typedef struct {
     int scale_log2;                  /* weights are integers in units of 2^-scale_log2 */
 } mnn_sample_info;
 
-#define MNN_SAMPLE_MAX_VOCAB (384 * 1024)
+#define MNN_SAMPLE_MAX_VOCAB (320 * 1024)
 /* Plan (host only); opts may be NULL = fp32, dense.  NULL on error: rows and vocab must be positive and row strides at least vocab
  * (MNN_EINVAL); vocab at most MNN_SAMPLE_MAX_VOCAB and rows at most 2^27 (MNN_EUNSUPPORTED). */
 MNN_API mnn_sample_plan_t mnn_sample_plan(int rows, int vocab, const mnn_sample_opts* opts);

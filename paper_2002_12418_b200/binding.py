@@ -38,7 +38,7 @@ NET_MAX_LAYERS = 128
 TYPES = {"fp32": 0, "bf16": 1, "fp16": 2}                                                # MNN_TYPE_*
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}                      # MNN_ACT_*
 RESIDUALS = {"none": 0, "after": 1, "before": 2}                                         # MNN_RESIDUAL_*
-SAMPLE_MAX_VOCAB = 384 * 1024
+SAMPLE_MAX_VOCAB = 320 * 1024
 
 
 class ConvOpts(ctypes.Structure):

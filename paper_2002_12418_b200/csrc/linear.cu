@@ -45,19 +45,15 @@ struct LinearParams {
 
 template <int TYPE, bool COPY>
 struct Roles {
-    // copier or converter warps; four where the epilogue's sums need the registers
-    static constexpr int kAux = TYPE == MNN_TYPE_FP32 ? 4 : COPY ? 8 : 0;
+    // copier or converter warps; four copiers where the epilogue's sums need the registers
+    static constexpr int kAux = COPY ? (TYPE == MNN_TYPE_FP32 ? 4 : 8) : (TYPE == MNN_TYPE_FP32 ? 8 : 0);
     static constexpr int kThreads = 64 + 32 * (kEpiWarps + kAux);
 };
 
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// lo = v - trunc(v) of the four values; an infinity's or NaN's is 0
-__device__ __forceinline__ float low_half(float v)
-{
-    const uint32_t b = __float_as_uint(v);
-    return (b & 0x7f800000u) == 0x7f800000u ? 0.0f : v - __uint_as_float(b & 0xffffe000u);
-}
+// lo = v - trunc(v) (no number for an infinity, which makes its sums none either: they are taken again)
+__device__ __forceinline__ float low_half(float v) { return v - __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
 __device__ __forceinline__ float4 low_half(float4 v) { return make_float4(low_half(v.x), low_half(v.y), low_half(v.z), low_half(v.w)); }
 
 // The 16 bytes at `at` of the tensor [begin, end), of which the first `valid` are wanted, the others zero.

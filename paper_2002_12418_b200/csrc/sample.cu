@@ -5,14 +5,22 @@
 // the running mass of what is kept, in index order, exceeds u times the whole.
 //
 // Every decision compares sums of weights with a border, so the sums have to be exact to well below one weight and must not
-// depend on the order in which threads add.  A weight is therefore computed in fp64 and held as a 64-bit integer in units of
-// 2^-scale (scale = 62 - log2 of the vocabulary, at most 52): sums are exact, in any order, and no atomic changes a result.
+// depend on the order in which threads add.  A weight is therefore evaluated in fp64 (relative error 5e-11) and held as an
+// integer in units of 2^-scale (scale = 62 - log2 of the vocabulary, at most 45): sums are exact, in any order, and no atomic
+// changes a result.
 //
-// A cluster of CTAs holds a row in shared memory (read once from HBM).  No sort: the border of a prefix is one value of l, found
-// by a histogram of counts and masses over 1024 bins of m - l (16 octaves of 64 bins, so that the bulk of a row spreads over many
-// bins whatever its scale and an outlier or a mask of the type's lowest value costs nothing), then, within the crossing bin, by
-// histograms over the range of its keys until one value is left.  Among equal values at the border the first ones by index are
-// kept.  The same histogram serves top-k (counts) and top-p (masses).
+// A cluster of CTAs holds a row in shared memory (read once from HBM).  No sort: the border of a prefix is one value of l.
+//   top-k: a histogram of counts over 1024 bins of m - l (16 octaves of 64 bins, so that the bulk of a row spreads over many bins
+//     whatever its scale, and an outlier or a mask of the type's lowest value costs nothing) gives the bin that holds it.
+//   top-p: the same counts, each times the weight in the middle of its bin, tell within a few bins where the border must lie.
+//     One pass then evaluates every weight once: those above that window are summed in registers, those inside go to 1024 finer
+//     bins.  (Only where the border turns out to lie elsewhere, a histogram of all masses is taken.)
+//   The few elements of the crossing bin are collected and ranked against each other; where there are many (ties by the thousand),
+//     histograms over the range of their keys narrow it down to one value.
+// Among equal values at the border the first ones by index are kept.
+//
+// Shared memory adds 32-bit integers in one instruction and 64-bit ones in a loop that retries, so masses are kept in three
+// planes of 15 bits of the weight: a CTA holds at most 2^17 elements, and no plane's sum passes 32 bits.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -32,6 +40,9 @@ typedef unsigned long long u64;
 constexpr int kBins = 1024;
 constexpr int kMaxWarps = 16;
 constexpr int kMaxCtas = 8;
+constexpr int kGather = 128;             // candidates that are ranked against each other instead of binned again
+constexpr int kMaxScale = 45;
+constexpr int kMostBytes = 176 * 1024;   // of a row's logits in one CTA: the largest vocabulary in fp32 over eight CTAs, and a step of rounding up
 
 template <int TYPE> struct Logit { typedef float T; static constexpr int kVec = 4; };
 template <> struct Logit<MNN_TYPE_BF16> { typedef __nv_bfloat16 T; static constexpr int kVec = 8; };
@@ -41,28 +52,25 @@ __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float widen(__half v) { return __half2float(v); }
 
-// Two zeros are one value and a NaN is no candidate.
-__device__ __forceinline__ float canonical(float v) { return v != v ? -INFINITY : v + 0.0f; }
-
 // An integer that orders as the values do.
 __device__ __forceinline__ uint32_t key_of(float v)
 {
     const uint32_t b = __float_as_uint(v);
     return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
 }
+__device__ __forceinline__ float value_of_key(uint32_t k) { return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k); }
 
-template <typename T>
-__device__ __forceinline__ T ld_cluster(const T* mine, uint32_t rank)
+__device__ __forceinline__ uint32_t ld_cluster(const uint32_t* mine, uint32_t rank)
 {
-    const uint32_t a = ptx::map_to_rank(ptx::smem_u32(mine), rank);
-    if (sizeof(T) == 8) {
-        u64 v;
-        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-        return (T)v;
-    }
     uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return (T)v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(ptx::map_to_rank(ptx::smem_u32(mine), rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ u64 ld_cluster(const u64* mine, uint32_t rank)
+{
+    u64 v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(ptx::map_to_rank(ptx::smem_u32(mine), rank)) : "memory");
+    return v;
 }
 
 __device__ __forceinline__ u64 warp_sum(u64 v)
@@ -71,40 +79,68 @@ __device__ __forceinline__ u64 warp_sum(u64 v)
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-template <typename T>
-__device__ __forceinline__ T warp_scan(T v, int lane)       // inclusive
+template <typename V>
+__device__ __forceinline__ V warp_scan(V v, int lane)       // inclusive
 {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const T t = __shfl_up_sync(0xffffffffu, v, o);
+        const V t = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += t;
     }
     return v;
 }
 
-struct Shared {
-    u64 mass[kBins];
-    uint32_t count[kBins];
-    u64 warp_mass[kMaxWarps];        // of this CTA, read by all
-    uint32_t warp_count[kMaxWarps];
-    float warp_max[kMaxWarps];
-    uint32_t key_min, key_max;       // of this CTA
-    float max;                       // of this CTA
-    // results of a step, for this CTA's threads
-    u64 scan_mass[kMaxWarps + 1];
-    u64 scan_count[kMaxWarps + 1];
-    int bin;
-    u64 above_mass, bin_mass;
-    uint32_t above_count, bin_count;
-};
+// 2^(d slope) with d slope <= 0, as an integer in units of 2^-scale, rounded to nearest.  2^r on [-1/2, 1/2] by 1 + r q(r) with q
+// of degree 6 (minimax by the exchange algorithm, relative error 4.7e-11); additions of 1.5 * 2^52 round to integers.  Every
+// operation is a named one: the sums of several passes are compared with each other, and a multiplication and an addition that
+// the compiler joins in one place and not in another would make two weights of one value.
+__device__ __forceinline__ u64 exp2_units(double d, double slope, int scale)
+{
+    constexpr double kRound = 6755399441055744.0;
+    const double y = __dmul_rn(d, slope);
+    const double t = __dadd_rn(y, kRound);
+    const double r = __dsub_rn(y, __dsub_rn(t, kRound));
+    double q = 1.5196158527772698e-05;
+    q = __fma_rn(q, r, 0.00015466756251326735);
+    q = __fma_rn(q, r, 0.0013333935047106663);
+    q = __fma_rn(q, r, 0.009618038132306056);
+    q = __fma_rn(q, r, 0.05550410366001406);
+    q = __fma_rn(q, r, 0.24022651066559253);
+    q = __fma_rn(q, r, 0.6931471807045294);
+    q = __fma_rn(q, r, 1.0);
+    // times 2^(n + scale): an addition to the exponent; the result is below 2^46
+    q = __hiloint2double(__double2hiint(q) + ((__double2loint(t) + scale) << 20), __double2loint(q));
+    return (u64)__double_as_longlong(__dadd_rn(q, 4503599627370496.0)) & 0xfffffffffffffull;
+}
 
-// The border of a prefix: everything above `key`, and the first `ties` with this key.
-struct Border {
-    uint32_t key;
-    u64 ties;
-    u64 mass_above;
-    uint32_t count_above;
-    bool any;                        // false: no border, everything is kept
+struct Shared {
+    uint32_t count[kBins];
+    uint32_t plane[3][kBins];        // masses by 15 bits: W & 0x7fff, (W >> 15) & 0x7fff, W >> 30
+    // merged over the cluster: running sums through the bins of this CTA's share
+    u64 run_mass[kBins];
+    uint32_t run_count[kBins];
+    u64 share_mass;
+    uint32_t share_count;
+    u64 scan_mass[kMaxWarps];
+    uint32_t scan_count[kMaxWarps];
+    float scan_estimate[kMaxWarps];
+    // sums of the warps' runs and of this CTA
+    u64 warp_mass[kMaxWarps], warp_above[kMaxWarps];
+    uint32_t warp_count[kMaxWarps];
+    u64 cta_mass, cta_above;
+    uint32_t cta_count;
+    float warp_max[kMaxWarps];
+    float max;                       // of this CTA
+    uint32_t key_min, key_max;       // of this CTA
+    uint32_t n_list;
+    uint32_t list[kGather];          // keys of this CTA's candidates that are to be ranked
+    uint32_t all[kGather];           // of the cluster's
+    u64 all_mass[kGather];
+    // what one warp found, for all
+    u64 found_mass, found_whole;
+    uint32_t found_count, found_key, found_equal;
+    int found_bin;
+    u64 ties_kept[kMaxWarps];
 };
 
 struct SampleParams {
@@ -114,7 +150,7 @@ struct SampleParams {
 };
 
 template <int TYPE>
-__global__ void __launch_bounds__(32 * kMaxWarps)
+__global__ void __launch_bounds__(32 * kMaxWarps, 2)
 sample_kernel(SampleParams p)
 {
     typedef typename Logit<TYPE>::T T;
@@ -128,405 +164,676 @@ sample_kernel(SampleParams p)
     __shared__ Shared sh;
     T* const held = reinterpret_cast<T*>(smem_raw);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_threads = blockDim.x;
+    const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31, n_threads = blockDim.x;
     const uint32_t rank = ptx::cluster_ctarank();
     uint32_t n_ctas;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
     const int row = blockIdx.x / n_ctas;
-    const int chunk = p.run * p.n_warps;
+    auto sync_row = [&]() {
+        if (n_ctas > 1) ptx::cluster_sync_all();
+        else __syncthreads();
+    };
+    auto clear = [&](bool masses) {
+        for (int i = threadIdx.x; i < kBins; i += n_threads) {
+            sh.count[i] = 0;
+            if (masses) sh.plane[0][i] = sh.plane[1][i] = sh.plane[2][i] = 0;
+        }
+    };
 
     ptx::grid_launch_dependents();
+    clear(true);
+    if (threadIdx.x == 0) sh.n_list = 0;
     ptx::grid_dependency_wait();
 
-    // ---- load.  Positions count from the 16-byte boundary at or before the row's first element.
+    // ---- load.  Positions count from the 16-byte boundary at or before the row's first element; every warp holds a run of them.
+    const int warp0 = warp * p.run;                                  // this warp's run in the CTA
+    const int cta0 = (int)rank * p.run * p.n_warps;                  // this CTA in the row
     const T* const row_ptr = static_cast<const T*>(p.a.logits) + (long long)row * p.ld;
     const int shift = (int)((reinterpret_cast<uintptr_t>(row_ptr) & 15u) / sizeof(T));
-    const T* const base = row_ptr - shift;
-    const int first = shift, last = shift + p.vocab;                 // positions [first, last) are the row
-    const int cta0 = (int)rank * chunk, warp0 = warp * p.run;        // of this CTA in the row, of this warp in the CTA
     float top = -INFINITY;
+    {
+        const T* const base = row_ptr - shift;
+        const int first = shift, last = shift + p.vocab;             // positions [first, last) are the row
 #pragma unroll 4
-    for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
-        const int at = cta0 + warp0 + i;
-        Piece q;
-        if (at >= first && at + VEC <= last) {
-            q.v = __ldg(reinterpret_cast<const uint4*>(base + at));
-        } else {
+        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+            const int at = cta0 + warp0 + i;
+            Piece q;
+            if (at >= first && at + VEC <= last) {
+                q.v = __ldg(reinterpret_cast<const uint4*>(base + at));
+            } else {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) q.e[j] = at + j >= first && at + j < last ? base[at + j] : (T)(-INFINITY);
+                for (int j = 0; j < VEC; ++j) q.e[j] = at + j >= first && at + j < last ? base[at + j] : (T)(-INFINITY);
+            }
+            *reinterpret_cast<uint4*>(held + warp0 + i) = q.v;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) top = fmaxf(top, widen(q.e[j]));       // fmaxf passes a NaN over
         }
-        *reinterpret_cast<uint4*>(held + warp0 + i) = q.v;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) top = fmaxf(top, widen(q.e[j]));           // fmaxf passes a NaN over
     }
     const float temperature = p.a.temperature ? p.a.temperature[row] : 1.0f;
     const int top_k = p.a.top_k ? p.a.top_k[row] : 0;
     const float top_p = p.a.top_p ? p.a.top_p[row] : 1.0f;
     const float min_p = p.a.min_p ? p.a.min_p[row] : 0.0f;
-    const bool greedy = !(temperature > 0.0f);
-    const bool by_count = greedy || (top_k > 0 && top_k < p.vocab), by_mass = !greedy && top_p < 1.0f;
-    const u64 k_target = greedy ? 1 : (u64)top_k;
+    const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
+    const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (lane == 0) sh.warp_max[warp] = top;
-    for (int i = threadIdx.x; i < kBins; i += n_threads) {
-        sh.mass[i] = 0;
-        sh.count[i] = 0;
-    }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < p.n_warps; ++i) top = fmaxf(top, sh.warp_max[i]);
-        sh.max = top;
+    if (warp == 0) {
+        top = lane < p.n_warps ? sh.warp_max[lane] : -INFINITY;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (lane == 0) sh.max = top;
     }
-    ptx::cluster_sync_all();
+    sync_row();
     float m = -INFINITY;
     for (uint32_t r = 0; r < n_ctas; ++r) m = fmaxf(m, __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(&sh.max), r)));
     m += 0.0f;                                                       // (one zero)
+    const bool some = m > -INFINITY;
 
-    // ---- weights
-    const double slope = greedy ? 0.0 : 1.4426950408889634074 / (double)temperature;      // log2(e) / T
-    const float cut = greedy ? 0.0f : -(float)(p.scale_log2 + 2) * 0.6931472f * temperature;    // below it a weight rounds to 0
-    auto exponent = [&](float l) { return ((double)l - (double)m) * slope; };              // log2 of the weight; l < m
+    // ---- weights.  Below `floor_l` they round to zero; with an infinite largest logit, or none but the first largest kept, all
+    // but its equals do.  (No branch: evaluations for several elements are to overlap.)
+    const bool m_inf = m == INFINITY;
+    const double slope = one ? 0.0 : 1.4426950408889634074 / (double)temperature;         // log2(e) / T
+    const float floor_l = m_inf || one ? m : m - (float)(p.scale_log2 + 3) * 0.6931472f * temperature;
+    const double m_wide = (double)m;
+    const u64 unit = 1ull << p.scale_log2;
     auto weight = [&](float l) -> u64 {
-        if (l == m) return 1ull << p.scale_log2;
-        if (m == INFINITY || !(l - m >= cut)) return 0;
-        return (u64)__double2ull_rn(exp2(exponent(l) + (double)p.scale_log2));
+        const double d = l == m ? 0.0 : __dsub_rn((double)fmaxf(l, floor_l), m_wide);
+        const u64 w = exp2_units(d, slope, p.scale_log2);
+        return l < floor_l ? 0 : w;
     };
-    auto value = [&](T e) { return canonical(widen(e)); };
-    auto for_each = [&](auto&& f) {                                  // every element that this warp holds
+    auto key = [&](float l) { return key_of(l + 0.0f); };            // (one key for both zeros)
+    // every element that this warp holds; what is no candidate is -infinity or NaN, and every test below is false for it
+    auto for_each = [&](auto&& f) {
         for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
             Piece q;
             q.v = *reinterpret_cast<const uint4*>(held + warp0 + i);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) f(value(q.e[j]));
+            for (int j = 0; j < VEC; ++j) f(widen(q.e[j]));
+        }
+    };
+    // the same by whole pieces, so that what is evaluated for several elements overlaps
+    auto for_each_piece = [&](auto&& f) {
+        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+            Piece q;
+            q.v = *reinterpret_cast<const uint4*>(held + warp0 + i);
+            float l[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) l[j] = widen(q.e[j]);
+            f(l);
         }
     };
     // 16 octaves of 64 bins of m - l, from 2^-10 to 2^6; what is nearer or further goes to the first or last bin
-    auto bin_of = [&](float l) {
-        const float d = l == m ? 0.0f : m - l;
-        return min(max((int)(__float_as_uint(d) >> 17) - ((127 - 10) << 6), 0), kBins - 1);
+    constexpr int kFirstBin = (127 - 10) << 6;                       // the bits of 2^-10, over 2^17
+    auto distance = [&](float l) { return l == m ? 0.0f : m - l; };
+    auto bin_of = [&](float l) { return min(max((int)(__float_as_uint(distance(l)) >> 17) - kFirstBin, 0), kBins - 1); };
+    auto add_mass = [&](int b, u64 w) {
+        const uint32_t w0 = (uint32_t)w & 0x7fffu, w1 = (uint32_t)(w >> 15) & 0x7fffu, w2 = (uint32_t)(w >> 30);
+        atomicAdd(&sh.plane[0][b], w0);
+        if (w1) atomicAdd(&sh.plane[1][b], w1);
+        if (w2) atomicAdd(&sh.plane[2][b], w2);
     };
 
-    // Sums the CTAs' histograms and finds the first bin at which the running count (or mass) reaches `target`, adding to what
-    // lies above.  Leaves the histograms zeroed.
-    auto crossing = [&](bool use_mass, u64 target, uint32_t count_above, u64 mass_above) {
-        ptx::cluster_sync_all();
-        constexpr int kPer = kBins / (32 * kMaxWarps);               // bins a thread of a full CTA takes
-        u64 bm[kPer * 8];
-        uint32_t bc[kPer * 8];
-        const int per = kBins / n_threads;                           // 2..8: CTAs have 4 to 16 warps
+    // What lies above the border that is being looked for, and the number of elements in the bin that holds it.
+    u64 above_mass = 0;
+    uint32_t above_count = 0, bin_count = 0;
+    int bin = -1;
+    // Sums the CTAs' histograms: each CTA takes a share of the bins.  Leaves them zeroed (for all after the next barrier).
+    const int log_share = 10 - (31 - __clz((int)n_ctas)), share = 1 << log_share;
+    auto merge = [&](bool masses) {
+        sync_row();
+        const int b0 = (int)rank * share, per = (share + n_threads - 1) / n_threads;
         u64 sum_m = 0;
         uint32_t sum_c = 0;
-#pragma unroll
-        for (int j = 0; j < kPer * 8; ++j) {
-            if (j >= per) break;
-            const int b = threadIdx.x * per + j;
-            u64 tm = 0;
-            uint32_t tc = 0;
-            for (uint32_t r = 0; r < n_ctas; ++r) {
-                tm += ld_cluster(&sh.mass[b], r);
-                tc += ld_cluster(&sh.count[b], r);
+        for (int j = 0; j < per; ++j) {
+            const int b = b0 + threadIdx.x * per + j;
+            if (b < b0 + share) {
+#pragma unroll 2
+                for (uint32_t r = 0; r < n_ctas; ++r) {
+                    sum_c += ld_cluster(&sh.count[b], r);
+                    if (masses)
+                        sum_m += (u64)ld_cluster(&sh.plane[0][b], r) + ((u64)ld_cluster(&sh.plane[1][b], r) << 15) + ((u64)ld_cluster(&sh.plane[2][b], r) << 30);
+                }
+                sh.run_mass[b] = sum_m;                              // (running within this thread; the rest is added below)
+                sh.run_count[b] = sum_c;
             }
-            bm[j] = tm;
-            bc[j] = tc;
-            sum_m += tm;
-            sum_c += tc;
         }
-        u64 scan_m = warp_scan(sum_m, lane);
-        u64 scan_c = warp_scan((u64)sum_c, lane);
+        const u64 scan_m = masses ? warp_scan(sum_m, lane) : 0;
+        const uint32_t scan_c = warp_scan(sum_c, lane);
         if (lane == 31) {
-            sh.scan_mass[warp + 1] = scan_m;
-            sh.scan_count[warp + 1] = scan_c;
-        }
-        if (threadIdx.x == 0) {
-            sh.scan_mass[0] = 0;
-            sh.scan_count[0] = 0;
-            sh.bin = -1;
+            sh.scan_mass[warp] = scan_m;
+            sh.scan_count[warp] = scan_c;
         }
         __syncthreads();
-        for (int i = 0; i <= warp; ++i) {
-            scan_m += sh.scan_mass[i];
-            scan_c += sh.scan_count[i];
+        u64 base_m = scan_m - sum_m;
+        uint32_t base_c = scan_c - sum_c;
+        for (int i = 0; i < warp; ++i) {
+            base_m += sh.scan_mass[i];
+            base_c += sh.scan_count[i];
         }
-        u64 run_m = mass_above + scan_m - sum_m;
-        u64 run_c = count_above + scan_c - sum_c;
-#pragma unroll
-        for (int j = 0; j < kPer * 8; ++j) {
-            if (j >= per) break;
-            const u64 before = use_mass ? run_m : run_c, after = before + (use_mass ? bm[j] : bc[j]);
-            if (before < target && after >= target) {
-                sh.bin = threadIdx.x * per + j;
-                sh.above_mass = run_m;
-                sh.above_count = (uint32_t)run_c;
-                sh.bin_mass = bm[j];
-                sh.bin_count = bc[j];
+        for (int j = 0; j < per; ++j) {
+            const int b = b0 + threadIdx.x * per + j;
+            if (b < b0 + share) {
+                sh.run_mass[b] += base_m;
+                sh.run_count[b] += base_c;
             }
-            run_m += bm[j];
-            run_c += bc[j];
         }
-        ptx::cluster_sync_all();                                     // (also: all have read this CTA's histograms)
-        for (int i = threadIdx.x; i < kBins; i += n_threads) {
-            sh.mass[i] = 0;
-            sh.count[i] = 0;
+        if (threadIdx.x == n_threads - 1) {
+            sh.share_mass = base_m + sum_m;
+            sh.share_count = base_c + sum_c;
         }
+        sync_row();                                                  // (all have read this CTA's histograms)
+        clear(masses);
     };
-    // Smallest and largest key of the elements that `in` takes, over the cluster.
-    auto key_range = [&](auto&& in, uint32_t* lo, uint32_t* hi) {
-        uint32_t mn = 0xffffffffu, mx = 0;
-        if (threadIdx.x == 0) {
-            sh.key_min = mn;
-            sh.key_max = mx;
+    // The first bin at which the running count (or mass) reaches `target`: found by one warp of each CTA, told to all.
+    auto cross = [&](bool use_mass, u64 target) {
+        if (warp == 0) {
+            u64 base_m = above_mass;
+            uint32_t base_c = above_count, count = 0;
+            int found = -1;
+            for (uint32_t r = 0; r < n_ctas && found < 0; ++r) {
+                const u64 sm = ld_cluster(&sh.share_mass, r);
+                const uint32_t sc = ld_cluster(&sh.share_count, r);
+                if (use_mass ? base_m + sm >= target : (u64)base_c + sc >= target) {
+                    u64 last_m = 0;                                  // of the 32 bins before
+                    uint32_t last_c = 0;
+                    for (int b0 = (int)r * share; found < 0 && b0 < ((int)r + 1) * share; b0 += 32) {
+                        const u64 rm = ld_cluster(&sh.run_mass[b0 + lane], r);
+                        const uint32_t rc = ld_cluster(&sh.run_count[b0 + lane], r);
+                        const unsigned hit = __ballot_sync(0xffffffffu, use_mass ? base_m + rm >= target : (u64)base_c + rc >= target);
+                        if (hit) {
+                            const int src = __ffs(hit) - 1;
+                            const u64 pm = __shfl_sync(0xffffffffu, rm, max(src - 1, 0));
+                            const uint32_t pc = __shfl_sync(0xffffffffu, rc, max(src - 1, 0)), cc = __shfl_sync(0xffffffffu, rc, src);
+                            last_m = src ? pm : last_m;
+                            last_c = src ? pc : last_c;
+                            found = b0 + src;
+                            count = cc - last_c;
+                        } else {
+                            last_m = __shfl_sync(0xffffffffu, rm, 31);
+                            last_c = __shfl_sync(0xffffffffu, rc, 31);
+                        }
+                    }
+                    base_m += last_m;
+                    base_c += last_c;
+                } else {
+                    base_m += sm;
+                    base_c += sc;
+                }
+            }
+            if (lane == 0) {
+                sh.found_bin = found;
+                sh.found_mass = base_m;
+                sh.found_count = base_c;
+                sh.found_equal = count;
+            }
         }
         __syncthreads();
-        for_each([&](float l) {
-            if (l > -INFINITY && in(l)) {
-                const uint32_t k = key_of(l);
-                mn = min(mn, k);
-                mx = max(mx, k);
-            }
-        });
-        mn = __reduce_min_sync(0xffffffffu, mn);
-        mx = __reduce_max_sync(0xffffffffu, mx);
-        if (lane == 0) {
-            atomicMin(&sh.key_min, mn);
-            atomicMax(&sh.key_max, mx);
+        bin = sh.found_bin;
+        if (bin >= 0) {
+            above_mass = sh.found_mass;
+            above_count = sh.found_count;
+            bin_count = sh.found_equal;
         }
-        ptx::cluster_sync_all();
-        mn = 0xffffffffu;
-        mx = 0;
-        for (uint32_t r = 0; r < n_ctas; ++r) {
-            mn = min(mn, ld_cluster(&sh.key_min, r));
-            mx = max(mx, ld_cluster(&sh.key_max, r));
-        }
-        ptx::cluster_sync_all();
-        *lo = mn;
-        *hi = mx;
+        __syncthreads();
     };
-    auto first_histogram = [&](bool masses) {
+    // Collects the keys of the n elements that `take` takes, in every CTA, with their weights if asked; their sum is returned.
+    auto collect = [&](int n, bool masses, auto&& take) -> u64 {
         for_each([&](float l) {
-            if (!(l > -INFINITY)) return;
-            const int b = bin_of(l);
-            atomicAdd(&sh.count[b], 1u);
-            if (masses) {
-                const u64 w = weight(l);
-                if (w) atomicAdd(&sh.mass[b], w);
-            }
+            if (take(l)) sh.list[atomicAdd(&sh.n_list, 1u)] = key(l);
         });
-    };
-    // The border at which the running count (or mass) reaches `target`; the histogram of the first level is in place.
-    auto find_border = [&](bool use_mass, bool masses, u64 target) {
-        Border b;
-        b.any = true;
-        crossing(use_mass, target, 0, 0);
-        uint32_t lo, hi;
-        int bin = sh.bin;
-        if (bin < 0) {                                               // fewer candidates than k: everything is kept
-            b.any = false;
-            return b;
+        sync_row();
+        u64 sum = 0;
+        for (int at = threadIdx.x; at < n; at += n_threads) {
+            int i = at;
+            uint32_t r = 0;
+            for (; r + 1 < n_ctas; ++r) {
+                const int have = (int)ld_cluster(&sh.n_list, r);
+                if (i < have) break;
+                i -= have;
+            }
+            const uint32_t k = ld_cluster(&sh.list[i], r);
+            const u64 w = masses ? weight(value_of_key(k)) : 0;
+            sh.all[at] = k;
+            sh.all_mass[at] = w;
+            sum += w;
         }
-        key_range([&](float l) { return bin_of(l) == bin; }, &lo, &hi);
-        while (lo != hi) {
-            const uint32_t span = hi - lo;
-            const int sh_bits = max(0, 32 - __clz(span) - 10);       // (hi - key) >> sh_bits < 1024
+        if (masses) {
+            sum = warp_sum(sum);
+            if (lane == 0) sh.scan_mass[warp] = sum;
+        }
+        sync_row();                                                  // (all have read this CTA's list)
+        if (threadIdx.x == 0) sh.n_list = 0;
+        if (masses) {
+            sum = 0;
+            for (int i = 0; i < p.n_warps; ++i) sum += sh.scan_mass[i];
+        }
+        return sum;
+    };
+    uint32_t border_key = 0, border_equal = 0;                       // the border, and how many elements are equal to it
+    // Of the n collected ones, the key at which the running count (or mass) reaches `target`.
+    auto ranked = [&](int n, bool use_mass, u64 target) {
+        // 2^g threads of a warp per key
+        int g = 0;
+        while (g < 5 && n << (g + 1) <= n_threads) ++g;
+        const int part = threadIdx.x & ((1 << g) - 1);
+        for (int i0 = 0; i0 < n; i0 += n_threads >> g) {
+            const int i = i0 + (threadIdx.x >> g);
+            const uint32_t k = sh.all[min(i, n - 1)];
+            u64 more = 0;
+            uint32_t more_c = 0, equal = 0;
+            for (int j = part; j < n; j += 1 << g) {
+                const uint32_t other = sh.all[j];
+                if (use_mass) more += other > k ? sh.all_mass[j] : 0;
+                more_c += other > k ? 1u : 0u;
+                equal += other == k ? 1u : 0u;
+            }
+            for (int o = 1 << g >> 1; o; o >>= 1) {
+                if (use_mass) more += __shfl_xor_sync(0xffffffffu, more, o);
+                more_c += __shfl_xor_sync(0xffffffffu, more_c, o);
+                equal += __shfl_xor_sync(0xffffffffu, equal, o);
+            }
+            const u64 before = use_mass ? above_mass + more : (u64)above_count + more_c;
+            const u64 here = use_mass ? (u64)equal * sh.all_mass[min(i, n - 1)] : (u64)equal;
+            if (part == 0 && i < n && before < target && before + here >= target) {  // (equals write the same)
+                sh.found_key = k;
+                sh.found_equal = equal;
+                sh.found_mass = above_mass + more;
+                sh.found_count = above_count + more_c;
+            }
+        }
+        __syncthreads();
+        above_mass = sh.found_mass;
+        above_count = sh.found_count;
+        border_key = sh.found_key;
+        border_equal = sh.found_equal;
+        __syncthreads();
+    };
+    // The border within the crossing bin, whose elements `in` takes.
+    auto narrow = [&](bool use_mass, u64 target, auto&& in) {
+        if (bin_count <= (uint32_t)kGather) {
+            const int n = (int)bin_count;
+            collect(n, use_mass, in);
+            ranked(n, use_mass, target);
+            return;
+        }
+        // many: the range of their keys, and a histogram over it, until one key is left
+        uint32_t lo = 0, hi = 0;
+        auto range = [&](auto&& take) {
+            uint32_t mn = 0xffffffffu, mx = 0;
+            if (threadIdx.x == 0) {
+                sh.key_min = mn;
+                sh.key_max = mx;
+            }
+            __syncthreads();
             for_each([&](float l) {
-                const uint32_t k = key_of(l);
-                if (l > -INFINITY && k >= lo && k <= hi) {
-                    atomicAdd(&sh.count[(hi - k) >> sh_bits], 1u);
-                    if (masses) {
-                        const u64 w = weight(l);
-                        if (w) atomicAdd(&sh.mass[(hi - k) >> sh_bits], w);
+                if (take(l)) {
+                    mn = min(mn, key(l));
+                    mx = max(mx, key(l));
+                }
+            });
+            mn = __reduce_min_sync(0xffffffffu, mn);
+            mx = __reduce_max_sync(0xffffffffu, mx);
+            if (lane == 0) {
+                atomicMin(&sh.key_min, mn);
+                atomicMax(&sh.key_max, mx);
+            }
+            sync_row();
+            lo = 0xffffffffu;
+            hi = 0;
+            for (uint32_t r = 0; r < n_ctas; ++r) {
+                lo = min(lo, ld_cluster(&sh.key_min, r));
+                hi = max(hi, ld_cluster(&sh.key_max, r));
+            }
+            sync_row();
+        };
+        range(in);
+        for (int level = 0; level < 4 && lo < hi; ++level) {          // (each divides the range by 1024)
+            const int drop = max(0, 22 - __clz(hi - lo));            // (hi - key) >> drop < 1024
+            const float v_lo = value_of_key(lo), v_hi = value_of_key(hi);
+            for_each([&](float l) {
+                if (l >= v_lo && l <= v_hi) {
+                    const int b = (int)((hi - key(l)) >> drop);
+                    atomicAdd(&sh.count[b], 1u);
+                    if (use_mass) add_mass(b, weight(l));
+                }
+            });
+            merge(use_mass);
+            cross(use_mass, target);
+            const uint32_t top_key = hi - ((uint32_t)max(bin, 0) << drop);
+            if (drop == 0 || bin < 0) {
+                lo = hi = top_key;
+            } else {
+                const float t_lo = value_of_key(max(lo, top_key - ((1u << drop) - 1u))), t_hi = value_of_key(top_key);
+                range([&](float l) { return l >= t_lo && l <= t_hi; });
+            }
+        }
+        border_key = lo;
+        border_equal = bin_count;
+    };
+
+    // ---- the border: everything above its value is kept, and the first `ties` equal to it
+    bool cut = some && one;
+    u64 ties = 1;
+    if (cut) border_key = key(m);
+    u64 run_above = 0;                                               // mass of what lies above `window_top` in this warp's run
+    float window_top = INFINITY;
+    if (some && (by_count || by_mass)) {
+        for_each([&](float l) {
+            if (l > -INFINITY) atomicAdd(&sh.count[bin_of(l)], 1u);
+        });
+        merge(false);
+        if (by_count) {
+            cross(false, (u64)top_k);
+            if (bin >= 0) {                                          // else fewer candidates than k: all are kept
+                const int b = bin;
+                narrow(false, (u64)top_k, [&](float l) { return l > -INFINITY && bin_of(l) == b; });
+                ties = (u64)top_k - above_count;
+                cut = true;
+            }
+        }
+    }
+    if (some && by_mass) {
+        // kept while the mass before < p * whole: up to where the running mass reaches ceil(p * whole)
+        auto border_target = [&](u64 whole) { return max(1ull, min((u64)ceil((double)fmaxf(top_p, 0.0f) * (double)whole), whole)); };
+        u64 target = 0;
+        bool done = false;
+        if (cut && above_count + border_equal <= (uint32_t)kGather) {            // few are left by top-k
+            const int n = (int)(above_count + border_equal);
+            const float from = value_of_key(border_key);
+            u64 whole = collect(n, true, [&](float l) { return l >= from; });
+            whole -= ((u64)n - (u64)top_k) * weight(from);
+            target = border_target(whole);
+            above_mass = 0;
+            above_count = 0;
+            ranked(n, true, target);
+            done = true;
+        } else if (!cut) {
+            // where the border must lie, by the counts and the weights in the middle of the bins
+            const float s = (float)slope;
+            auto middle = [&](int b) { return b == 0 ? 1.0f : exp2f(-s * __uint_as_float((uint32_t)((b + kFirstBin) << 17) + (1u << 16))); };
+            auto estimate = [&](int b) {
+                const uint32_t r = (uint32_t)(b >> log_share), c = ld_cluster(&sh.run_count[b], r);
+                return (float)(c - (b & (share - 1) ? ld_cluster(&sh.run_count[b - 1], r) : 0u)) * middle(b);
+            };
+            const int per = kBins / n_threads;
+            float part = 0.0f;
+            for (int j = 0; j < per; ++j) part += estimate(threadIdx.x * per + j);
+            float run = warp_scan(part, lane);
+            if (lane == 31) sh.scan_estimate[warp] = run;
+            if (threadIdx.x == 0) sh.found_bin = kBins - 1;
+            __syncthreads();
+            run -= part;
+            float guess = 0.0f;
+            for (int i = 0; i < p.n_warps; ++i) {
+                if (i < warp) run += sh.scan_estimate[i];
+                guess += sh.scan_estimate[i];
+            }
+            guess *= fmaxf(top_p, 0.0f);
+            if (run <= guess && run + part > guess)
+                for (int j = 0; j < per; ++j) {
+                    run += estimate(threadIdx.x * per + j);
+                    if (run > guess || j + 1 == per) {
+                        sh.found_bin = threadIdx.x * per + j;
+                        break;
+                    }
+                }
+            __syncthreads();
+            const int w0 = max(sh.found_bin - 1, 0), w1 = min(sh.found_bin + 2, kBins - 1);
+            const uint32_t bits0 = (uint32_t)(w0 + kFirstBin) << 17;
+            const float d0 = w0 ? __uint_as_float(bits0) : 0.0f;
+            const float d1 = w1 == kBins - 1 ? INFINITY : __uint_as_float((uint32_t)(w1 + 1 + kFirstBin) << 17);
+            // 1024 finer bins over the window of four
+            auto fine = [&](float d) { return min(max((int)(__float_as_uint(d) - bits0) >> 9, 0), kBins - 1); };
+            u64 sum_above = 0, sum = 0;
+            for_each_piece([&](const float (&l)[VEC]) {
+                u64 w[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[j] = weight(l[j]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float d = distance(l[j]);
+                    const u64 here = l[j] >= floor_l ? w[j] : 0;     // (a NaN's weight is none)
+                    sum += here;
+                    if (d < d0) {
+                        sum_above += here;
+                    } else if (d < d1 && here) {
+                        const int b = fine(d);
+                        atomicAdd(&sh.count[b], 1u);
+                        add_mass(b, here);
                     }
                 }
             });
-            const uint32_t above_c = sh.above_count;
-            const u64 above_m = sh.above_mass;
-            crossing(use_mass, target, above_c, above_m);
-            bin = sh.bin;
-            const uint32_t top_key = hi - ((uint32_t)bin << sh_bits);
-            if (sh_bits == 0) {
-                lo = hi = top_key;
-            } else {
-                const uint32_t b_lo = max(lo, top_key - ((1u << sh_bits) - 1u)), b_hi = top_key;
-                key_range([&](float l) {
-                    const uint32_t k = key_of(l);
-                    return k >= b_lo && k <= b_hi;
-                }, &lo, &hi);
+            run_above = warp_sum(sum_above);
+            sum = warp_sum(sum);
+            if (lane == 0) {
+                sh.warp_above[warp] = run_above;
+                sh.warp_mass[warp] = sum;
             }
-        }
-        b.key = lo;
-        b.mass_above = sh.above_mass;
-        b.count_above = sh.above_count;
-        b.ties = sh.bin_count;                                       // (all of them; the caller cuts)
-        return b;
-    };
-    auto value_of_key = [](uint32_t k) { return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k); };
-
-    Border border;
-    border.any = false;
-    if (m > -INFINITY) {
-        u64 whole = 0;                                               // mass of what top-k leaves
-        if (by_count || by_mass) {
             __syncthreads();
-            first_histogram(by_mass);
-        }
-        if (by_count) {
-            border = find_border(false, by_mass, k_target);
-            if (border.any) {
-                const u64 ties = k_target - border.count_above;      // 1.. of the border's equals
-                border.ties = ties;
-                if (by_mass) whole = border.mass_above + ties * weight(value_of_key(border.key));
+            if (warp == 0) {
+                const u64 a = warp_sum(lane < p.n_warps ? sh.warp_above[lane] : 0), b = warp_sum(lane < p.n_warps ? sh.warp_mass[lane] : 0);
+                if (lane == 0) {
+                    sh.cta_above = a;
+                    sh.cta_mass = b;
+                }
             }
-            if (by_mass) {
-                __syncthreads();
-                first_histogram(true);                               // again: the search used the bins up
+            merge(true);
+            u64 whole = 0;
+            above_mass = 0;
+            above_count = 0;
+            for (uint32_t r = 0; r < n_ctas; ++r) {
+                above_mass += ld_cluster(&sh.cta_above, r);
+                whole += ld_cluster(&sh.cta_mass, r);
+            }
+            target = border_target(whole);
+            if (above_mass < target) {
+                cross(true, target);
+                done = bin >= 0;
+            }
+            if (done) {
+                window_top = d0;
+                // the fine bin as an interval of distances
+                const float b0 = bin ? __uint_as_float(bits0 + ((uint32_t)bin << 9)) : d0;
+                const float b1 = bin < kBins - 1 ? __uint_as_float(bits0 + ((uint32_t)(bin + 1) << 9)) : d1;
+                narrow(true, target, [&](float l) {
+                    const float d = distance(l);
+                    return d >= b0 && d < b1 && weight(l) != 0;
+                });
+            } else {
+                sync_row();                                          // (the histograms are zero again for all)
             }
         }
-        if (by_mass) {
-            if (!border.any) {                                       // the whole row's mass
-                u64 sum = 0;
-                ptx::cluster_sync_all();
-                for (int i = threadIdx.x; i < kBins; i += n_threads)
-                    for (uint32_t r = 0; r < n_ctas; ++r) sum += ld_cluster(&sh.mass[i], r);
-                sum = warp_sum(sum);
-                if (lane == 0) sh.warp_mass[warp] = sum;
-                __syncthreads();
-                for (int i = 0; i < p.n_warps; ++i) whole += sh.warp_mass[i];
-            }
-            // kept while the mass before < p * whole: up to where the running mass reaches ceil(p * whole)
-            const double want = ceil((double)fmaxf(top_p, 0.0f) * (double)whole);
-            const u64 target = max(1ull, min((u64)want, whole));
-            border = find_border(true, true, target);
-            const u64 w = weight(value_of_key(border.key));
-            border.ties = (target - border.mass_above + w - 1) / w;
+        if (!done) {                                                 // a histogram of all masses from top-k's border on
+            const float from = cut ? value_of_key(border_key) : -INFINITY;
+            const u64 surplus = cut ? (u64)(above_count + border_equal) - (u64)top_k : 0;      // equals of that border that do not count
+            for_each([&](float l) {
+                if (l >= from && l > -INFINITY) {
+                    const int b = bin_of(l);
+                    atomicAdd(&sh.count[b], 1u);
+                    add_mass(b, weight(l));
+                }
+            });
+            merge(true);
+            u64 whole = 0;
+            for (uint32_t r = 0; r < n_ctas; ++r) whole += ld_cluster(&sh.share_mass, r);
+            if (surplus) whole -= surplus * weight(from);
+            target = border_target(whole);
+            above_mass = 0;
+            above_count = 0;
+            cross(true, target);
+            const int b = bin;
+            narrow(true, target, [&](float l) { return l >= from && l > -INFINITY && bin_of(l) == b; });
         }
+        const u64 w = weight(value_of_key(border_key));
+        ties = (target - above_mass + w - 1) / w;
+        cut = true;
     }
 
     // ---- draw: masses of the warps' runs, then the run that holds the border, then the element
-    const float border_value = border.any ? value_of_key(border.key) : -INFINITY;
-    const u64 least = min_p > 0.0f ? max(1ull, (u64)ceil((double)fminf(min_p, 1.0f) * (double)(1ull << p.scale_log2))) : 0;
-    const bool border_counts = border.any && m > -INFINITY && weight(border_value) >= least;
-    auto above = [&](float l) { return border.any ? l > border_value : l > -INFINITY; };
+    const float border_value = cut ? value_of_key(border_key) : -INFINITY;
+    const u64 least = min_p > 0.0f ? max(1ull, (u64)ceil((double)fminf(min_p, 1.0f) * (double)unit)) : 0;
+    const u64 border_w = cut ? weight(border_value) : 0;
+    const bool equals_count = cut && border_w >= least;
+    auto kept_above = [&](float l) -> u64 {                          // the weight of an element above the border, if min-p keeps it
+        const u64 w = weight(l);
+        return w >= least ? w : 0;
+    };
     u64 mass = 0;
     uint32_t equals = 0;
-    if (m > -INFINITY)
-        for_each([&](float l) {
-            if (above(l)) {
-                const u64 w = weight(l);
-                if (w >= least) mass += w;
+    if (window_top < INFINITY && equals_count) {                     // what lies above the window is summed already, and min-p keeps it
+        mass = lane == 0 ? run_above : 0;
+        for_each_piece([&](const float (&l)[VEC]) {
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                any = any || (l[j] > border_value && distance(l[j]) >= window_top);
+                equals += l[j] == border_value ? 1u : 0u;
             }
-            equals += border_counts && l == border_value ? 1u : 0u;
+            if (any) {
+                u64 w[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[j] = weight(l[j]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) mass += l[j] > border_value && distance(l[j]) >= window_top ? w[j] : 0;
+            }
         });
+    } else if (some) {
+        const float from = fmaxf(border_value, floor_l);
+        for_each_piece([&](const float (&l)[VEC]) {
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                any = any || l[j] >= from;
+                equals += equals_count && l[j] == border_value ? 1u : 0u;
+            }
+            if (any) {
+                u64 w[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) mass += l[j] >= from && l[j] > border_value ? w[j] : 0;
+            }
+        });
+    }
     mass = warp_sum(mass);
     equals = __reduce_add_sync(0xffffffffu, equals);
-    __syncthreads();                                                 // (warp_mass is read above)
     if (lane == 0) {
         sh.warp_mass[warp] = mass;
         sh.warp_count[warp] = equals;
     }
-    ptx::cluster_sync_all();
-    // every warp: prefix over the runs before its own, and the whole
-    const u64 border_w = border_counts ? weight(border_value) : 0;
-    u64 total = 0, before = 0, mine = 0, ties_mine = 0;
-    {
-        u64 seen = 0;                                                // equals so far
-        const int runs = (int)n_ctas * p.n_warps, own = (int)rank * p.n_warps + warp;
-        for (int i0 = 0; i0 < runs; i0 += 32) {
-            const int i = i0 + lane;
-            u64 rm = 0;
-            u64 rc = 0;
-            if (i < runs) {
-                rm = ld_cluster(&sh.warp_mass[i % p.n_warps], i / p.n_warps);
-                rc = ld_cluster(&sh.warp_count[i % p.n_warps], i / p.n_warps);
-            }
-            const u64 c_incl = warp_scan(rc, lane), c_before = seen + c_incl - rc;
-            const u64 ties = border_counts && c_before < border.ties ? min(rc, border.ties - c_before) : 0;
-            const u64 v = rm + ties * border_w;
-            const u64 v_incl = warp_scan(v, lane);
-            if (own >= i0 && own < i0 + 32) {
-                before = total + __shfl_sync(0xffffffffu, v_incl - v, own - i0);
-                mine = __shfl_sync(0xffffffffu, v, own - i0);
-                ties_mine = __shfl_sync(0xffffffffu, ties, own - i0);
-            }
-            total += __shfl_sync(0xffffffffu, v_incl, 31);
-            seen += __shfl_sync(0xffffffffu, c_incl, 31);
+    __syncthreads();
+    u64 run_mass = 0, run_count = 0;                                 // lane i of warp 0: of warp i's run
+    if (warp == 0) {
+        run_mass = lane < p.n_warps ? sh.warp_mass[lane] : 0;
+        run_count = lane < p.n_warps ? sh.warp_count[lane] : 0;
+        const u64 a = warp_sum(run_mass), b = warp_sum(run_count);
+        if (lane == 0) {
+            sh.cta_mass = a;
+            sh.cta_count = (uint32_t)b;
         }
     }
-    const double whole_kept = (double)total;
-    auto share = [&](float l) {                                      // weight / kept mass
-        const double w = l == m ? 1.0 : m == INFINITY ? 0.0 : exp2(exponent(l));
-        return (float)(ldexp(w, p.scale_log2) / whole_kept);
+    sync_row();
+    auto share_of = [&](float l, double whole) {                     // weight / kept mass
+        const double w = l == m ? 1.0 : m_inf ? 0.0 : exp2(((double)l - m_wide) * slope);
+        return (float)(w * (double)unit / whole);
     };
-    const float u_row = p.a.u[row];
-    const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f; // (a NaN counts as 0)
-    const u64 target = min((u64)((double)u * whole_kept), total - 1);
-    if (total == 0) {                                                // no candidate
-        if (rank == 0 && threadIdx.x == 0) {
-            p.a.token[row] = -1;
-            if (p.a.prob) p.a.prob[row] = 0.0f;
-        }
-    } else if (target >= before && target < before + mine) {         // one warp of the cluster
-        u64 left = target - before, ties_left = ties_mine;
-        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
-            Piece q;
-            q.v = *reinterpret_cast<const uint4*>(held + warp0 + i);
-            uint32_t eq = 0;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) eq += border_counts && value(q.e[j]) == border_value ? 1u : 0u;
-            const uint32_t eq_incl = warp_scan(eq, lane);
-            u64 ties_lane = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;    // that may still be kept from here on
-            u64 wv[VEC], sum = 0;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float l = value(q.e[j]);
-                u64 w = 0;
-                if (above(l)) {
-                    w = weight(l);
-                    if (w < least) w = 0;
-                } else if (border_counts && l == border_value && ties_lane > 0) {
-                    w = border_w;
-                    --ties_lane;
-                }
-                wv[j] = w;
-                sum += w;
+    if (warp == 0) {
+        // the CTAs' sums, with as many equals as still count
+        const u64 c_m = lane < (int)n_ctas ? ld_cluster(&sh.cta_mass, (uint32_t)lane) : 0;
+        const u64 c_c = lane < (int)n_ctas ? ld_cluster(&sh.cta_count, (uint32_t)lane) : 0;
+        const u64 cta_seen = warp_scan(c_c, lane) - c_c;
+        const u64 c_v = c_m + (cta_seen < ties ? min(c_c, ties - cta_seen) : 0) * border_w;
+        const u64 c_incl = warp_scan(c_v, lane);
+        const u64 total = __shfl_sync(0xffffffffu, c_incl, 31);
+        // and this CTA's runs
+        const u64 seen = __shfl_sync(0xffffffffu, cta_seen, (int)rank) + warp_scan(run_count, lane) - run_count;
+        const u64 ties_run = seen < ties ? min(run_count, ties - seen) : 0;
+        const u64 v = run_mass + ties_run * border_w;
+        const u64 before = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank) + warp_scan(v, lane) - v;
+        if (lane < p.n_warps) sh.ties_kept[lane] = ties_run;
+        if (lane == 0) sh.found_whole = total;
+        if (total == 0) {                                            // no candidate
+            if (rank == 0 && lane == 0) {
+                p.a.token[row] = -1;
+                if (p.a.prob) p.a.prob[row] = 0.0f;
             }
-            const u64 incl = warp_scan(sum, lane);
-            const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
-            if (hit) {
-                if (lane == __ffs(hit) - 1) {
-                    u64 rest = left - (incl - sum);
-                    bool found = false;
+        } else {
+            const float u_row = p.a.u[row];
+            const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;     // (a NaN counts as 0)
+            const u64 target = min((u64)((double)u * (double)total), total - 1);
+            const unsigned owner = __ballot_sync(0xffffffffu, target >= before && target < before + v);
+            if (owner) {                                             // one run of the cluster
+                const int src = __ffs(owner) - 1, run0 = src * p.run;
+                u64 left = target - __shfl_sync(0xffffffffu, before, src), ties_left = __shfl_sync(0xffffffffu, ties_run, src);
+                for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+                    Piece q;
+                    q.v = *reinterpret_cast<const uint4*>(held + run0 + i);
+                    uint32_t eq = 0;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        if (!found && rest < wv[j]) {
-                            found = true;
-                            p.a.token[row] = cta0 + warp0 + i + j - shift;
-                            if (p.a.prob) p.a.prob[row] = share(value(q.e[j]));
+                    for (int j = 0; j < VEC; ++j) eq += equals_count && widen(q.e[j]) == border_value ? 1u : 0u;
+                    const uint32_t eq_incl = warp_scan(eq, lane);
+                    // the weight of an element, where this lane's first `lane_ties` equals of the border still count
+                    const u64 lane_ties = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;
+                    auto kept_weight = [&](float l, u64 w, u64& t) -> u64 {
+                        if (l > border_value) return w;
+                        if (equals_count && l == border_value && t > 0) {
+                            --t;
+                            return border_w;
                         }
-                        rest -= wv[j];
+                        return 0;
+                    };
+                    u64 sum = 0, t = lane_ties, w[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) w[j] = kept_above(widen(q.e[j]));
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) sum += kept_weight(widen(q.e[j]), w[j], t);
+                    const u64 incl = warp_scan(sum, lane);
+                    const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
+                    if (hit) {
+                        if (lane == __ffs(hit) - 1) {
+                            u64 rest = left - (incl - sum);
+                            bool found = false;
+                            t = lane_ties;
+#pragma unroll 1
+                            for (int j = 0; j < VEC && !found; ++j) {
+                                const float l = widen(held[run0 + i + j]);
+                                const u64 here = kept_weight(l, kept_above(l), t);
+                                if (rest < here) {
+                                    found = true;
+                                    p.a.token[row] = cta0 + run0 + i + j - shift;
+                                    if (p.a.prob) p.a.prob[row] = share_of(l, (double)total);
+                                }
+                                rest -= here;
+                            }
+                        }
+                        break;
                     }
+                    left -= __shfl_sync(0xffffffffu, incl, 31);
+                    const uint32_t eq_all = __shfl_sync(0xffffffffu, eq_incl, 31);
+                    ties_left = ties_left > eq_all ? ties_left - eq_all : 0;
                 }
-                break;
             }
-            left -= __shfl_sync(0xffffffffu, incl, 31);
-            const uint32_t eq_all = __shfl_sync(0xffffffffu, eq_incl, 31);
-            ties_left = ties_left > eq_all ? ties_left - eq_all : 0;
         }
     }
     if (p.a.probs) {                                                 // the whole filtered distribution
+        __syncthreads();
         float* const out = p.a.probs + (long long)row * p.ld_probs;
-        u64 ties_left = ties_mine;
+        u64 ties_left = sh.ties_kept[warp];
+        const double whole = (double)sh.found_whole;
         for (int i = lane; i < p.run; i += 32) {
             const int at = cta0 + warp0 + i - shift;
-            const float l = value(held[warp0 + i]);
-            const bool eq = border_counts && l == border_value;
+            const float l = widen(held[warp0 + i]);
+            const bool eq = equals_count && l == border_value;
             const unsigned eqs = __ballot_sync(0xffffffffu, eq);
-            const bool keep = above(l) ? (least == 0 || weight(l) >= least) : eq && (u64)__popc(eqs & ((1u << lane) - 1u)) < ties_left;
-            if (at >= 0 && at < p.vocab) out[at] = keep && total ? share(l) : 0.0f;
+            const bool keep = l > border_value ? (least == 0 || weight(l) >= least) : eq && (u64)__popc(eqs & ((1u << lane) - 1u)) < ties_left;
+            if (at >= 0 && at < p.vocab) out[at] = keep && whole > 0.0 ? share_of(l, whole) : 0.0f;
             const u64 n = (u64)__popc(eqs);
             ties_left = ties_left > n ? ties_left - n : 0;
         }
     }
-    ptx::cluster_sync_all();                                         // nobody leaves while its sums are being read
+    sync_row();                                                      // nobody leaves while its sums are being read
 }
 
 template <int TYPE>
@@ -534,7 +841,7 @@ cudaError_t run_sample(const SampleShape& s, const SampleTiling& t, const Sample
 {
     static unsigned long long done = 0;
     const int bytes = t.run * t.warps * (TYPE == MNN_TYPE_FP32 ? 4 : 2);
-    cudaError_t e = allow_smem_once(reinterpret_cast<const void*>(sample_kernel<TYPE>), 208 * 1024, &done);
+    cudaError_t e = allow_smem_once(reinterpret_cast<const void*>(sample_kernel<TYPE>), kMostBytes, &done);
     if (e != cudaSuccess) return e;
     return launch_cluster(t.ctas, sample_kernel<TYPE>, dim3((unsigned)(s.rows * t.ctas)), dim3(32 * t.warps), (size_t)bytes, stream, p);
 }
@@ -545,20 +852,20 @@ SampleTiling sample_tiling(const SampleShape& s, int num_sms)
 {
     SampleTiling t;
     const int size = s.type == MNN_TYPE_FP32 ? 4 : 2, vec = 16 / size;
-    const int capacity = 200 * 1024 / size;                          // elements a CTA holds
     const long long span = (long long)s.vocab + vec - 1;             // with the positions before an unaligned row
-    // CTAs per row: as many as the row needs, and more while that leaves SMs idle and every CTA 4096 elements
+    // CTAs per row: as many as leave each 64 KB, so that two are resident per SM, and more while SMs idle and every CTA keeps
+    // 4096 elements
     t.ctas = 1;
-    while (t.ctas < kMaxCtas && ((span + t.ctas - 1) / t.ctas > capacity ||
-                                 ((long long)s.rows * t.ctas * 2 <= 2ll * num_sms && span / (2 * t.ctas) >= 4096)))
+    while (t.ctas < kMaxCtas && ((span + t.ctas - 1) / t.ctas * size > 66 * 1024 ||
+                                 ((long long)s.rows * t.ctas <= num_sms && span / (2 * t.ctas) >= 4096)))
         t.ctas *= 2;
     const long long per_cta = (span + t.ctas - 1) / t.ctas;
-    t.warps = per_cta > 8192 ? 16 : per_cta > 2048 ? 8 : 4;
+    t.warps = per_cta > 2048 ? 16 : 8;
     const int step = 32 * vec;
     t.run = (int)((per_cta + (long long)t.warps * step - 1) / ((long long)t.warps * step)) * step;
     int bits = 0;
     while ((1ll << bits) < s.vocab) ++bits;
-    t.scale_log2 = 62 - bits < 52 ? 62 - bits : 52;
+    t.scale_log2 = 62 - bits < kMaxScale ? 62 - bits : kMaxScale;
     return t;
 }
 

@@ -26,7 +26,7 @@ struct SampleArgs {
 };
 
 // The largest vocabulary that a cluster holds.
-constexpr int kSampleMaxVocab = 384 * 1024;
+constexpr int kSampleMaxVocab = 320 * 1024;
 
 SampleTiling sample_tiling(const SampleShape& s, int num_sms);
 cudaError_t launch_sample(const SampleShape& s, const SampleTiling& t, const SampleArgs& a, cudaStream_t stream);
