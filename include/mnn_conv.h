@@ -395,14 +395,17 @@ MNN_API void mnn_net_destroy(mnn_net_t net);
  * elements are contiguous, rows may be any number of elements apart that is not smaller than their length.  Sums, bias,
  * activation and residual are evaluated in fp32 and rounded once, at the store.  fp32 operands enter as TF32 halves (hi*hi +
  * lo*hi + hi*lo, about 22 bits of mantissa); 16-bit operands as they are.  An infinity or NaN in x or w gives what the
- * definition gives.  Pointers need the alignment of their element only; 16-byte aligned x and w with row strides of a multiple of
- * 16 bytes are copied by TMA, others by a slower kernel.  y may be the residual itself (same pointer and stride) and must not
- * overlap x, w or bias.  No operand is transformed ahead: one launch per run, for one row as for thousands.
+ * definition gives.  Pointers need the alignment of their element only; x and w on 16-byte boundaries with row strides of a multiple
+ * of 16 bytes are read directly, others shifted on the way.  y may be the residual itself (same pointer and stride) and must not
+ * overlap x, w or bias.  Nothing is prepared ahead or kept from one run for the next.
  * Rules on pointers, streams and errors as for the convolutions; the current device must be the device of `stream`.
  */
 enum { MNN_TYPE_FP32 = 0, MNN_TYPE_BF16 = 1, MNN_TYPE_FP16 = 2 };
 /* GELU: v (1 + erf(v / sqrt 2)) / 2;  GELU_TANH: v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2;  SILU: v / (1 + e^-v) */
 enum { MNN_ACT_NONE = 0, MNN_ACT_RELU = 1, MNN_ACT_GELU = 2, MNN_ACT_GELU_TANH = 3, MNN_ACT_SILU = 4 };
+/* Kernels: TILES 128 features x 16..256 rows of x on one SM; PAIRS 256 x 128..256 on two; COPIED as TILES for rows that are not 16-byte
+ * aligned; FEW up to four rows of x, without tensor cores */
+enum { MNN_LINEAR_TILES = 0, MNN_LINEAR_PAIRS = 1, MNN_LINEAR_COPIED = 2, MNN_LINEAR_FEW = 3 };
 enum { MNN_RESIDUAL_NONE = 0, MNN_RESIDUAL_AFTER = 1, MNN_RESIDUAL_BEFORE = 2 };
 
 typedef struct mnn_linear_plan_s* mnn_linear_plan_t;   /* opaque host object */
@@ -417,16 +420,19 @@ typedef struct {
 
 typedef struct {
     int M, N, K, type, act, residual;
-    int pair;                        /* 1: the kernel on pairs of SMs (256 features x 256 rows per work item) */
-    int copy;                        /* 1: rows are not 16-byte aligned and are fetched by warps instead of TMA */
-    int rows_per_item;               /* rows of x per work item; it has 128 features (256 on pairs) */
-    int split;                       /* CTAs of a cluster that share an item's K loop */
+    int form;                        /* MNN_LINEAR_* for x and w on 16-byte boundaries */
+    int rows_per_item;               /* rows of x per work item */
+    int features_per_item;
+    int split;                       /* CTAs of a cluster (FEW: warps of a CTA) that share an item's K loop */
+    int launches_per_run;            /* 2 where PAIRS lays operands out in the workspace first */
+    int reserved;
     long long items;
-    long long workspace_bytes;       /* the status word */
+    long long workspace_bytes;       /* the status word, and what PAIRS lays out */
 } mnn_linear_info;
 
 /* Plan one product (host only, needs no GPU); opts may be NULL = fp32, dense, no activation, no residual.  NULL on error:
- * M, N and K must be positive and row strides at least the row length (MNN_EINVAL); tensors below 2^40 elements. */
+ * M, N and K must be positive and row strides at least the row length (MNN_EINVAL); M, N and K up to 2^28, tensors below 2^40
+ * elements (MNN_EUNSUPPORTED). */
 MNN_API mnn_linear_plan_t mnn_linear_plan(int M, int N, int K, const mnn_linear_opts* opts);
 MNN_API int mnn_linear_plan_query(mnn_linear_plan_t plan, mnn_linear_info* info);
 /* Hand over the caller-owned workspace (>= info.workspace_bytes, 1024-byte aligned) and clear its status word. */

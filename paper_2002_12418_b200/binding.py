@@ -38,6 +38,7 @@ NET_MAX_LAYERS = 128
 TYPES = {"fp32": 0, "bf16": 1, "fp16": 2}                                                # MNN_TYPE_*
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}                      # MNN_ACT_*
 RESIDUALS = {"none": 0, "after": 1, "before": 2}                                         # MNN_RESIDUAL_*
+LINEAR_TILES, LINEAR_PAIRS, LINEAR_COPIED, LINEAR_FEW = 0, 1, 2, 3
 SAMPLE_MAX_VOCAB = 320 * 1024
 
 
@@ -89,8 +90,9 @@ class LinearOpts(ctypes.Structure):
 
 class LinearInfo(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int), ("N", ctypes.c_int), ("K", ctypes.c_int), ("type", ctypes.c_int), ("act", ctypes.c_int),
-                ("residual", ctypes.c_int), ("pair", ctypes.c_int), ("copy", ctypes.c_int), ("rows_per_item", ctypes.c_int),
-                ("split", ctypes.c_int), ("items", ctypes.c_longlong), ("workspace_bytes", ctypes.c_longlong)]
+                ("residual", ctypes.c_int), ("form", ctypes.c_int), ("rows_per_item", ctypes.c_int), ("features_per_item", ctypes.c_int),
+                ("split", ctypes.c_int), ("launches_per_run", ctypes.c_int), ("reserved", ctypes.c_int), ("items", ctypes.c_longlong),
+                ("workspace_bytes", ctypes.c_longlong)]
 
 
 class SampleOpts(ctypes.Structure):
@@ -591,12 +593,12 @@ class _RowRunner:
     def stream(self) -> int:
         return self._raw_stream()
 
-    def _rows(self, t, shape, ld, what, dtype=None):
-        """The address of a tensor of `shape` whose rows are ld elements apart."""
-        if t.dtype is not (dtype or self.dtype) or t.device != self.device or t.shape != shape:
-            raise MnnError(MNN_EINVAL, "%s must be a %s tensor of shape %s on %s" % (what, dtype or self.dtype, tuple(shape), self.device))
-        if shape[1] > 1 and t.stride(1) != 1 or shape[0] > 1 and t.stride(0) != ld:
-            raise MnnError(MNN_EINVAL, "rows of %s must be contiguous and %d elements apart" % (what, ld))
+    def _rows(self, t, shape, strides, what, dtype):
+        """The address of a tensor of `shape` whose rows lie as `strides` says."""
+        if t.dtype is not dtype or t.device != self.device or t.shape != shape:
+            raise MnnError(MNN_EINVAL, "%s must be a %s tensor of shape %s on %s" % (what, dtype, tuple(shape), self.device))
+        if t.stride() != strides and (shape[1] > 1 and t.stride(1) != 1 or shape[0] > 1 and t.stride(0) != strides[0]):
+            raise MnnError(MNN_EINVAL, "rows of %s must be contiguous and %d elements apart" % (what, strides[0]))
         return t.data_ptr()
 
     def _vector(self, t, shape, what, dtype):
@@ -609,7 +611,7 @@ class _RowRunner:
     def _launch(self, call, *args):
         """The library's call with this runner's device as the current one."""
         torch = self.torch
-        if torch.cuda.current_device() == self.device.index:
+        if torch._C._cuda_getDevice() == self.device.index:
             rc = call(self.plan, *args, self._raw_stream())
         else:
             with torch.cuda.device(self.device):
@@ -634,23 +636,26 @@ class LinearRunner(_RowRunner):
         torch = self.torch
         self.plan = mnn_linear_plan(M, N, K, make_linear_opts(dtype, act, residual, ldx, ldw, ldy, ldr))
         self.info = mnn_linear_plan_query(self.plan)
+        self._M, self._N, self._ld_y = M, N, ldy or N
         self._x, self._w, self._y, self._n = torch.Size((M, K)), torch.Size((N, K)), torch.Size((M, N)), torch.Size((N,))
-        self._ldx, self._ldw, self._ldy, self._ldr = ldx or K, ldw or K, ldy or N, ldr or N
+        self._sx, self._sw, self._sy, self._sr = (ldx or K, 1), (ldw or K, 1), (ldy or N, 1), (ldr or N, 1)
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(self.info.workspace_bytes + 1024, dtype=torch.uint8, device=self.device)
             self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
             mnn_linear_set_workspace(self.plan, self._ws_ptr, self.info.workspace_bytes)
 
     def run(self, x, w, bias=None, residual=None, y=None):
+        dtype = self.dtype
         if y is None:
-            if self._ldy == self._y[1]:
-                y = self.torch.empty(self._y, dtype=self.dtype, device=self.device)
-            else:
-                y = self.torch.empty((self._y[0], self._ldy), dtype=self.dtype, device=self.device)[:, :self._y[1]]
-        self._launch(_lib.mnn_linear_run, self._rows(x, self._x, self._ldx, "x"), self._rows(w, self._w, self._ldw, "w"),
-                     self._vector(bias, self._n, "bias", self.dtype),
-                     self._rows(residual, self._y, self._ldr, "residual") if residual is not None else None,
-                     self._rows(y, self._y, self._ldy, "y"))
+            y = self.torch.empty(self._M, self._ld_y, dtype=dtype, device=self.device)
+            if self._ld_y != self._N:
+                y = y[:, :self._N]
+            y_ptr = y.data_ptr()
+        else:
+            y_ptr = self._rows(y, self._y, self._sy, "y", dtype)
+        self._launch(_lib.mnn_linear_run, self._rows(x, self._x, self._sx, "x", dtype), self._rows(w, self._w, self._sw, "w", dtype),
+                     self._vector(bias, self._n, "bias", dtype),
+                     self._rows(residual, self._y, self._sr, "residual", dtype) if residual is not None else None, y_ptr)
         return y
 
     def device_status(self) -> int:
@@ -670,7 +675,8 @@ class SampleRunner(_RowRunner):
         super().__init__(dtype, device)
         self.plan = mnn_sample_plan(rows, vocab, make_sample_opts(dtype, ld))
         self.info = mnn_sample_plan_query(self.plan)
-        self._logits, self._n, self._ld = self.torch.Size((rows, vocab)), self.torch.Size((rows,)), ld or vocab
+        self._rows_n, self._vocab = rows, vocab
+        self._logits, self._n, self._sl, self._sp = self.torch.Size((rows, vocab)), self.torch.Size((rows,)), (ld or vocab, 1), (vocab, 1)
 
     def run(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, probs=False, token=None, prob=None):
         """probs: True for the whole filtered distribution too, or the tensor to write it to."""
@@ -678,20 +684,25 @@ class SampleRunner(_RowRunner):
         f = torch.float32
         if u is None:
             raise MnnError(MNN_EINVAL, "u is required")
+        n = self._n
         if token is None:
-            token = torch.empty(self._n, dtype=torch.int32, device=self.device)
+            token = torch.empty(self._rows_n, dtype=torch.int32, device=self.device)
+            token_ptr = token.data_ptr()
+        else:
+            token_ptr = self._vector(token, n, "token", torch.int32)
         if prob is None:
-            prob = torch.empty(self._n, dtype=f, device=self.device)
+            prob = torch.empty(self._rows_n, dtype=f, device=self.device)
+            prob_ptr = prob.data_ptr()
+        else:
+            prob_ptr = self._vector(prob, n, "prob", f)
         if probs is True:
-            probs = torch.empty(self._logits, dtype=f, device=self.device)
+            probs = torch.empty(self._rows_n, self._vocab, dtype=f, device=self.device)
         elif probs is False:
             probs = None
-        n = self._n
-        self._launch(_lib.mnn_sample_run, self._rows(logits, self._logits, self._ld, "logits"), self._vector(u, n, "u", f),
+        self._launch(_lib.mnn_sample_run, self._rows(logits, self._logits, self._sl, "logits", self.dtype), self._vector(u, n, "u", f),
                      self._vector(temperature, n, "temperature", f), self._vector(top_k, n, "top_k", torch.int32),
-                     self._vector(top_p, n, "top_p", f), self._vector(min_p, n, "min_p", f),
-                     self._vector(token, n, "token", torch.int32), self._vector(prob, n, "prob", f),
-                     self._rows(probs, self._logits, self._logits[1], "probs", f) if probs is not None else None)
+                     self._vector(top_p, n, "top_p", f), self._vector(min_p, n, "min_p", f), token_ptr, prob_ptr,
+                     self._rows(probs, self._logits, self._sp, "probs", f) if probs is not None else None)
         return token, prob, probs
 
     def close(self) -> None:

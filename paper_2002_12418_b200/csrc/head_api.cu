@@ -20,7 +20,8 @@ struct mnn_linear_plan_s {
     int act, residual, num_sms;
     LinearTiling tiling;             // by the row strides
     LinearTiling unaligned;          // where a run's x or w does not start on a 16-byte boundary
-    int* status = nullptr;
+    char* ws = nullptr;              // status word, then the operands laid out anew
+    long long workspace_bytes = 0;
 };
 
 struct mnn_sample_plan_s {
@@ -30,7 +31,7 @@ struct mnn_sample_plan_s {
 
 namespace {
 
-constexpr long long kLinearWorkspace = 1024;
+constexpr long long kStatusBytes = 1024;   // head of the workspace: device status word
 
 int type_bytes(int type) { return type == MNN_TYPE_FP32 ? 4 : 2; }
 bool known_type(int type) { return type >= MNN_TYPE_FP32 && type <= MNN_TYPE_FP16; }
@@ -76,6 +77,10 @@ mnn_linear_plan_t mnn_linear_plan(int M, int N, int K, const mnn_linear_opts* op
         report_error(MNN_EINVAL, "a row stride is smaller than the row");
         return nullptr;
     }
+    if (M > (1 << 28) || N > (1 << 28) || K > (1 << 28)) {
+        report_error(MNN_EUNSUPPORTED, "M, N and K may be up to 2^28");
+        return nullptr;
+    }
     const long long most = 1ll << 40;
     if (o.ldx >= most / M || o.ldw >= most / N || o.ldy >= most / M || o.ldr >= most / M) {
         report_error(MNN_EUNSUPPORTED, "tensor too large");
@@ -92,6 +97,7 @@ mnn_linear_plan_t mnn_linear_plan(int M, int N, int K, const mnn_linear_opts* op
     p->num_sms = (int)current_calibration().c[7];
     p->tiling = linear_tiling(p->s, false, p->num_sms);
     p->unaligned = linear_tiling(p->s, true, p->num_sms);
+    p->workspace_bytes = kStatusBytes + (p->tiling.relay_bytes > p->unaligned.relay_bytes ? p->tiling.relay_bytes : p->unaligned.relay_bytes);
     return p;
 }
 
@@ -101,25 +107,26 @@ int mnn_linear_plan_query(mnn_linear_plan_t p, mnn_linear_info* info)
     std::memset(info, 0, sizeof(*info));
     info->M = p->s.M; info->N = p->s.N; info->K = p->s.K;
     info->type = p->s.type; info->act = p->act; info->residual = p->residual;
-    info->pair = p->tiling.pair;
-    info->copy = p->tiling.copy;
+    info->form = p->tiling.form;
     info->rows_per_item = p->tiling.bm;
+    info->features_per_item = p->tiling.feats;
     info->split = p->tiling.split;
+    info->launches_per_run = p->tiling.relay ? 2 : 1;
     info->items = p->tiling.items;
-    info->workspace_bytes = kLinearWorkspace;
+    info->workspace_bytes = p->workspace_bytes;
     return MNN_OK;
 }
 
 int mnn_linear_set_workspace(mnn_linear_plan_t p, void* workspace, long long bytes)
 {
     if (!p) return report_error(MNN_EINVAL, "NULL plan");
-    p->status = nullptr;
+    p->ws = nullptr;
     if (!workspace) return report_error(MNN_EWORKSPACE, "the plan needs a workspace");
-    if (bytes < kLinearWorkspace) return report_error(MNN_EWORKSPACE, "workspace smaller than info.workspace_bytes");
+    if (bytes < p->workspace_bytes) return report_error(MNN_EWORKSPACE, "workspace smaller than info.workspace_bytes");
     if (!aligned(workspace, 1024)) return report_error(MNN_EALIGN, "workspace must be 1024-byte aligned");
     cudaError_t e = cudaMemset(workspace, 0, sizeof(int));
     if (e != cudaSuccess) return report_cuda_error(e, "clearing the status word");
-    p->status = static_cast<int*>(workspace);
+    p->ws = static_cast<char*>(workspace);
     return MNN_OK;
 }
 
@@ -128,7 +135,7 @@ int mnn_linear_run(mnn_linear_plan_t p, const void* x, const void* w, const void
     if (!p || !x || !w || !y) return report_error(MNN_EINVAL, "NULL argument");
     if ((p->residual != MNN_RESIDUAL_NONE) != (residual != nullptr))
         return report_error(MNN_EINVAL, p->residual ? "the plan has a residual and none was given" : "a residual was given and the plan has none");
-    if (!p->status) return report_error(MNN_EWORKSPACE, "call mnn_linear_set_workspace first");
+    if (!p->ws) return report_error(MNN_EWORKSPACE, "call mnn_linear_set_workspace first");
     const int eb = type_bytes(p->s.type);
     if (!aligned(x, eb) || !aligned(w, eb) || !aligned(y, eb) || !aligned(bias, eb) || !aligned(residual, eb))
         return report_error(MNN_EALIGN, "a tensor is not aligned to its elements");
@@ -142,8 +149,11 @@ int mnn_linear_run(mnn_linear_plan_t p, const void* x, const void* w, const void
     const LinearTiling& t = aligned(x, 16) && aligned(w, 16) ? p->tiling : p->unaligned;
     const LinearEpilogue epi = {bias, residual, y, p->s.ldr, p->s.ldy, p->act, p->residual};
     const char* why = "launching the matrix product";
-    cudaError_t e = t.pair ? launch_linear_pair(p->s, t, p->num_sms, x, w, epi, p->status, static_cast<cudaStream_t>(stream), &why)
-                           : launch_linear(p->s, t, p->num_sms, x, w, epi, p->status, static_cast<cudaStream_t>(stream), &why);
+    int* const status = reinterpret_cast<int*>(p->ws);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = t.form == MNN_LINEAR_FEW     ? launch_linear_few(s, t, x, w, epi, st)
+                    : t.form == MNN_LINEAR_PAIRS ? launch_linear_pair(s, t, p->num_sms, x, w, epi, status, p->ws + kStatusBytes, st, &why)
+                                                 : launch_linear(s, t, p->num_sms, x, w, epi, status, p->ws + kStatusBytes, st, &why);
     return e == cudaSuccess ? MNN_OK : report_cuda_error(e, why);
 }
 
@@ -151,13 +161,13 @@ int mnn_linear_device_status(mnn_linear_plan_t p, void* stream, int* code)
 {
     if (!p || !code) return report_error(MNN_EINVAL, "NULL plan or code");
     *code = 0;
-    if (!p->status) return MNN_OK;
+    if (!p->ws) return MNN_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = cudaMemcpyAsync(code, p->status, sizeof(int), cudaMemcpyDeviceToHost, st);
+    cudaError_t e = cudaMemcpyAsync(code, p->ws, sizeof(int), cudaMemcpyDeviceToHost, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) return report_cuda_error(e, "reading the status word");
     if (*code != 0) {
-        e = cudaMemsetAsync(p->status, 0, sizeof(int), st);
+        e = cudaMemsetAsync(p->ws, 0, sizeof(int), st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
         if (e != cudaSuccess) return report_cuda_error(e, "clearing the status word");
     }

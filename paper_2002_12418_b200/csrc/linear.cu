@@ -20,6 +20,7 @@
 // shift neighbours together and write the swizzled tile themselves.
 #include "cluster.cuh"
 #include "linear_epilogue.cuh"
+#include "linear_piece.cuh"
 #include "kernels.h"
 #include "umma.cuh"
 
@@ -51,43 +52,6 @@ struct Roles {
 };
 
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// lo = v - trunc(v) (no number for an infinity, which makes its sums none either: they are taken again)
-__device__ __forceinline__ float low_half(float v) { return v - __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
-__device__ __forceinline__ float4 low_half(float4 v) { return make_float4(low_half(v.x), low_half(v.y), low_half(v.z), low_half(v.w)); }
-
-// The 16 bytes at `at` of the tensor [begin, end), of which the first `valid` are wanted, the others zero.
-template <int EB>
-__device__ __forceinline__ uint4 load_piece(const char* at, int valid, const char* begin, const char* end)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(at);
-    const char* lo = at - (a & 15u);
-    if (valid >= 16 && (a & 15u) == 0) return __ldg(reinterpret_cast<const uint4*>(at));
-    if (valid >= 16 && lo >= begin && lo + 32 <= end) {
-        const uint4 p = __ldg(reinterpret_cast<const uint4*>(lo)), q = __ldg(reinterpret_cast<const uint4*>(lo) + 1);
-        uint32_t u0 = p.x, u1 = p.y, u2 = p.z, u3 = p.w, u4 = q.x, u5 = q.y, u6 = q.z;
-        if (a & 8u) { u0 = u2; u1 = u3; u2 = u4; u3 = u5; u4 = u6; u5 = q.w; u6 = 0; }
-        if (a & 4u) { u0 = u1; u1 = u2; u2 = u3; u3 = u4; u4 = u5; }
-        if (EB == 2 && (a & 2u)) {
-            u0 = __funnelshift_r(u0, u1, 16);
-            u1 = __funnelshift_r(u1, u2, 16);
-            u2 = __funnelshift_r(u2, u3, 16);
-            u3 = __funnelshift_r(u3, u4, 16);
-        }
-        return make_uint4(u0, u1, u2, u3);
-    }
-    uint32_t u[4] = {0, 0, 0, 0};
-    if (EB == 4) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j * 4 < valid) u[j] = __ldg(reinterpret_cast<const uint32_t*>(at) + j);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j * 2 < valid) u[j >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(at) + j) << ((j & 1) * 16);
-    }
-    return make_uint4(u[0], u[1], u[2], u[3]);
-}
 
 // TYPE: MNN_TYPE_*; COPY: operands fetched by copier warps; SPLIT: clusters share K loops; KB: blocks of K (128 bytes a row) per
 // stage.
@@ -276,16 +240,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
                 const long long m0 = m_item + ch * 16;
                 const int rows = (int)min(16ll, p.M - m0);
-                if (F32 && n_ok) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j < rows && !isfinite(s[j])) {
-                            const float *xr = static_cast<const float*>(p.x) + (m0 + j) * p.ldx, *wr = static_cast<const float*>(p.w) + (long long)n * p.ldw;
-                            float t = 0.0f;
-                            for (int k = 0; k < p.K; ++k) t = fmaf(xr[k], wr[k], t);
-                            s[j] = t;
-                        }
-                }
+                if (F32 && n_ok) retake_sums<16>(s, rows, m0, n, static_cast<const float*>(p.x), p.ldx, static_cast<const float*>(p.w), p.ldw, p.K);
                 out.store(p.epi, s, bias, m0, rows, n, n_ok);
             };
             if (F32) {
@@ -436,14 +391,10 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 ptx::cluster_reduce_columns(smem_base, p.bm, rank, p.split, row, (warp - 2) >> 2, kEpiWarps >> 2, [&](int c, float sum) {
                     const long long m = (long long)mb * p.bm + c;
                     if (m >= p.M) return;
-                    if (F32 && !isfinite(sum)) {
-                        const float *xr = static_cast<const float*>(p.x) + m * p.ldx, *wr = static_cast<const float*>(p.w) + (long long)n * p.ldw;
-                        sum = 0.0f;
-                        for (int k = 0; k < p.K; ++k) sum = fmaf(xr[k], wr[k], sum);
-                    }
                     LinearStore<TYPE, 1> out;
                     out.fetch(p.epi, m, 1, n, true);
                     float s[1] = {sum};
+                    if (F32) retake_sums<1>(s, 1, m, n, static_cast<const float*>(p.x), p.ldx, static_cast<const float*>(p.w), p.ldw, p.K);
                     out.store(p.epi, s, bias, m, 1, n, true);
                 });
         }
@@ -487,7 +438,7 @@ cudaError_t run_variant(const LinearTiling& t, LinearParams& p, int num_sms, con
 template <int TYPE, int KB>
 cudaError_t run_type(const LinearTiling& t, LinearParams& p, int num_sms, const CUtensorMap& mx, const CUtensorMap& mw, cudaStream_t stream)
 {
-    if (t.copy) return t.split > 1 ? run_variant<TYPE, true, true, 1>(t, p, num_sms, mx, mw, stream) : run_variant<TYPE, true, false, 1>(t, p, num_sms, mx, mw, stream);
+    if (t.form == MNN_LINEAR_COPIED) return t.split > 1 ? run_variant<TYPE, true, true, 1>(t, p, num_sms, mx, mw, stream) : run_variant<TYPE, true, false, 1>(t, p, num_sms, mx, mw, stream);
     return t.split > 1 ? run_variant<TYPE, false, true, KB>(t, p, num_sms, mx, mw, stream) : run_variant<TYPE, false, false, KB>(t, p, num_sms, mx, mw, stream);
 }
 
@@ -509,20 +460,43 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
 {
     const bool f32 = s.type == MNN_TYPE_FP32;
     const int eb = f32 ? 4 : 2;
+    const bool strides = (s.ldx * eb) % 16 != 0 || (s.ldw * eb) % 16 != 0, copy = unaligned || strides;
     LinearTiling t = {};
-    t.copy = unaligned || (s.ldx * eb) % 16 != 0 || (s.ldw * eb) % 16 != 0;
-    // Estimated clocks: waves of CTAs, each its share of K blocks at the slower of the tensor core (4096 multiply-adds of 16 bits
-    // a clock; TF32 half of that, three products) and the delivery of the tiles (about 48 bytes a clock and SM), plus start and end.
+    if (s.M <= 4) {
+        // up to four rows: a stream of w (linear_few.cu); two features a warp, and one, and several warps per K loop, where that
+        // leaves fewer than 16 warps per SM
+        t.form = MNN_LINEAR_FEW;
+        t.bm = s.M;
+        t.feats = s.N / 2 >= 16ll * num_sms ? 2 : 1;
+        t.items = (s.N + t.feats - 1) / t.feats;
+        t.split = 1;
+        while (t.split < 8 && t.items * t.split < 16ll * num_sms && (long long)s.K * eb >= 1024ll * t.split) t.split *= 2;
+        return t;
+    }
+    // Estimated clocks of the tile kernel: waves of CTAs, each its share of K blocks at the slower of the tensor core (4096
+    // multiply-adds of 16 bits a clock; TF32 a third of that, three products) and the delivery of the tiles (about 48 bytes a clock
+    // and SM by TMA, 3 by copier warps), plus start and end.  Rows whose strides TMA cannot copy are laid out anew first, at
+    // about 20 bytes a clock and SM; where only a tensor's start is not aligned no workspace is kept for that, and copier warps
+    // fetch it (64 x 4097 x 4096 BF16: 79 us by them).
+    t.form = copy && !strides ? MNN_LINEAR_COPIED : MNN_LINEAR_TILES;
+    t.feats = kTileF;
     const long long fblocks = (s.N + kTileF - 1) / kTileF, kblocks = ((long long)s.K * eb + 127) / 128;
+    const double operand_bytes = ((double)s.M + s.N) * s.K * eb;
+    t.relay = strides;
+    if (t.relay) {
+        t.ld_relay = ((long long)s.K * eb + 15) / 16 * 16 / eb;
+        t.relay_bytes = (s.M + (long long)s.N) * t.ld_relay * eb;
+    }
+    const double tile_relay = t.relay ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
     double best = 0;
     for (int bm = 16; bm <= (f32 ? 128 : 256); bm *= 2) {
         if (bm > 16 && bm / 2 >= s.M) break;
         const long long items = fblocks * ((s.M + bm - 1) / bm);
         for (int split = 1; split <= 8; split *= 2) {
             if (split > 1 && (items * split > num_sms || kblocks < 2 * split)) break;
-            const double mma = f32 ? 6.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.copy ? 16.0 : 48.0);
+            const double mma = f32 ? 9.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.form == MNN_LINEAR_COPIED ? 3.0 : 48.0);
             const long long waves = (items * split + num_sms - 1) / num_sms;
-            const double clocks = waves * ((kblocks + split - 1) / split * (mma > load ? mma : load)) + 1500.0 + 8.0 * bm + (split > 1 ? 1200.0 + 6.0 * bm : 0.0);
+            const double clocks = waves * ((kblocks + split - 1) / split * (mma > load ? mma : load)) + 1500.0 + 8.0 * bm + (split > 1 ? 1200.0 + 6.0 * bm : 0.0) + tile_relay;
             if (best == 0 || clocks < best) {
                 best = clocks;
                 t.bm = bm;
@@ -531,22 +505,31 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
             }
         }
     }
-    // pairs of SMs: half the rows of x per CTA, so that the tensor core and not the delivery decides
-    if (!f32 && !t.copy) {
-        const long long items = ((s.N + 255) / 256) * (long long)((s.M + 255) / 256), pairs = num_sms / 2;
-        const double clocks = (double)((items + pairs - 1) / pairs) * (kblocks * 660.0) + 3500.0;
+    // Pairs of SMs (linear_pair.cu): half the rows of x per CTA, so that the tensor core and not the delivery decides.  fp32 (as
+    // two FP16 halves, three products) needs a pass over both operands first, as rows that are not aligned do.
+    if (s.M < 192 || t.form == MNN_LINEAR_COPIED) return t;
+    const long long ld = ((long long)s.K + 7) / 8 * 8, blocks = ((long long)s.K + 63) / 64;
+    const double relay = strides || f32 ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
+    for (int bm = 256; bm >= 128; bm -= 32) {
+        const long long items = ((s.N + 255) / 256) * (long long)((s.M + bm - 1) / bm), pairs = num_sms / 2;
+        const double clocks = (double)((items + pairs - 1) / pairs) * (blocks * (f32 ? 7.8 : 2.6) * bm + 1000.0) + 3500.0 + relay;
         if (clocks < best) {
-            t.pair = 1;
-            t.bm = 256;
+            best = clocks;
+            t.form = MNN_LINEAR_PAIRS;
+            t.feats = 256;
+            t.bm = bm;
             t.split = 1;
             t.items = items;
+            t.relay = strides || f32;
+            t.ld_relay = ld;
+            t.relay_bytes = t.relay ? (s.M + (long long)s.N) * (f32 ? 4 * ld + 4 : 2 * ld) : 0;
         }
     }
     return t;
 }
 
 cudaError_t launch_linear(const LinearShape& s, const LinearTiling& t, int num_sms, const void* x, const void* w,
-                          const LinearEpilogue& epi, int* status, cudaStream_t stream, const char** why)
+                          const LinearEpilogue& epi, int* status, void* relay, cudaStream_t stream, const char** why)
 {
     LinearParams p = {};
     p.M = s.M; p.N = s.N; p.K = s.K;
@@ -560,7 +543,17 @@ cudaError_t launch_linear(const LinearShape& s, const LinearTiling& t, int num_s
     p.status = status;
     const int eb = s.type == MNN_TYPE_FP32 ? 4 : 2;
     CUtensorMap mx = {}, mw = {};
-    if (!t.copy && (!encode_rows_map(&mx, x, eb, s.K, s.M, s.ldx, t.bm) || !encode_rows_map(&mw, w, eb, s.K, s.N, s.ldw, kTileF))) {
+    const void *xs = x, *ws = w;
+    long long ldx = s.ldx, ldw = s.ldw;
+    if (t.relay) {
+        const LinearRelayed rx = {x, s.M, s.ldx, relay, nullptr, nullptr}, rw = {w, s.N, s.ldw, static_cast<char*>(relay) + s.M * t.ld_relay * eb, nullptr, nullptr};
+        cudaError_t e = launch_linear_relay(rx, rw, s.K, eb, t.ld_relay, num_sms, stream);
+        if (e != cudaSuccess) return e;
+        xs = rx.same;
+        ws = rw.same;
+        ldx = ldw = t.ld_relay;
+    }
+    if (t.form != MNN_LINEAR_COPIED && (!encode_rows_map(&mx, xs, eb, s.K, s.M, ldx, t.bm) || !encode_rows_map(&mw, ws, eb, s.K, s.N, ldw, kTileF))) {
         *why = "cuTensorMapEncodeTiled failed or is unavailable";
         return cudaErrorInvalidValue;
     }

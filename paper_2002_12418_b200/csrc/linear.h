@@ -21,20 +21,34 @@ struct LinearShape {
 
 // How a product is cut: decided from sizes and alignment alone, ahead of any run.
 struct LinearTiling {
-    int pair;        // 1: pairs of SMs on 256 features x 256 rows (linear_pair.cu)
-    int copy;        // 1: rows that do not start on 16-byte boundaries, fetched by warps instead of TMA
-    int bm;          // rows of x per work item (MMA N): 16..256; a work item has 128 features (pair: 256)
-    int split;       // CTAs of a cluster that share a work item's K loop
+    int form;            // MNN_LINEAR_*
+    int bm;              // rows of x per work item
+    int feats;           // features per work item
+    int split;           // CTAs of a cluster (MNN_LINEAR_FEW: warps of a CTA) that share a work item's K loop
     long long items;
+    bool relay;          // the operands are laid out anew first (linear_relay.cu)
+    long long ld_relay;  // elements between rows there (of halves: fp32 on pairs)
+    long long relay_bytes;
 };
 
 // unaligned: x or w does not start on a 16-byte boundary.
 LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms);
 
+// An operand that is laid out anew: src -> same; fp32 on pairs: src -> high halves (same), low halves and the exponents of the rows' scales.
+struct LinearRelayed {
+    const void* src;
+    long long rows, ld;              // ld: elements between rows of src
+    void *same, *low;
+    int* up;
+};
+
+// `relay`: relay_bytes of device memory.
 cudaError_t launch_linear(const LinearShape& s, const LinearTiling& t, int num_sms, const void* x, const void* w,
-                          const LinearEpilogue& epi, int* status, cudaStream_t stream, const char** why);
+                          const LinearEpilogue& epi, int* status, void* relay, cudaStream_t stream, const char** why);
+cudaError_t launch_linear_few(const LinearShape& s, const LinearTiling& t, const void* x, const void* w, const LinearEpilogue& epi, cudaStream_t stream);
 cudaError_t launch_linear_pair(const LinearShape& s, const LinearTiling& t, int num_sms, const void* x, const void* w,
-                               const LinearEpilogue& epi, int* status, cudaStream_t stream, const char** why);
+                               const LinearEpilogue& epi, int* status, void* relay, cudaStream_t stream, const char** why);
+cudaError_t launch_linear_relay(const LinearRelayed& x, const LinearRelayed& w, int K, int elem_bytes, long long ld_out, int num_sms, cudaStream_t stream);
 
 // 2-D map over rows of k_len elements, ld elements apart; box = box_rows rows of 128 bytes in the 128-byte swizzle; what lies
 // outside reads as zero.

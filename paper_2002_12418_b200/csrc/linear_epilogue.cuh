@@ -90,6 +90,20 @@ struct LinearStore {
     }
 };
 
+// fp32: sums without a finite value are taken again, term by term (an infinity's low half is no number).
+template <int NUM>
+__device__ __forceinline__ void retake_sums(float (&s)[NUM], int rows, long long m0, int n, const float* x, long long ldx, const float* w, long long ldw, int K)
+{
+#pragma unroll
+    for (int j = 0; j < NUM; ++j)
+        if (j < rows && !isfinite(s[j])) {
+            const float *xr = x + (m0 + j) * ldx, *wr = w + (long long)n * ldw;
+            float t = 0.0f;
+            for (int k = 0; k < K; ++k) t = fmaf(xr[k], wr[k], t);
+            s[j] = t;
+        }
+}
+
 template <int TYPE>
 __device__ __forceinline__ float linear_bias(const LinearEpilogue& e, int n, bool n_ok)
 {

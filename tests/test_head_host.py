@@ -17,7 +17,7 @@ def linear(*a, **kw):
 
 
 def test_struct_layouts_match_the_header():
-    assert ctypes.sizeof(B.LinearOpts) == 4 * 4 + 4 * 8 and ctypes.sizeof(B.LinearInfo) == 10 * 4 + 2 * 8
+    assert ctypes.sizeof(B.LinearOpts) == 4 * 4 + 4 * 8 and ctypes.sizeof(B.LinearInfo) == 12 * 4 + 2 * 8
     assert ctypes.sizeof(B.SampleOpts) == 2 * 4 + 2 * 8 and ctypes.sizeof(B.SampleInfo) == 6 * 4
 
 
@@ -61,17 +61,27 @@ def test_linear_refuses_runs():
 
 
 def test_linear_plans():
-    one = linear(1, 4096, 4096, dtype="bf16")
-    assert one.rows_per_item == 16 and one.split > 1 and not one.copy and not one.pair and one.workspace_bytes == 1024
-    assert linear(8192, 8192, 4096, dtype="bf16").pair and not linear(8192, 8192, 4096, dtype="fp32").pair
-    assert linear(64, 64, 1001, dtype="bf16").copy and linear(64, 64, 1001, dtype="bf16", ldx=1008, ldw=1008).copy == 0
-    assert linear(64, 64, 1002, dtype="fp32").copy
-    for M in (1, 2, 16, 17, 100, 1000):
+    few = linear(1, 4096, 4096, dtype="bf16")
+    assert few.form == B.LINEAR_FEW and few.workspace_bytes == 1024 and few.launches_per_run == 1
+    one = linear(8, 4096, 4096, dtype="bf16")
+    assert one.form == B.LINEAR_TILES and one.rows_per_item == 16 and one.split > 1 and one.launches_per_run == 1
+    big = linear(8192, 8192, 4096, dtype="bf16")
+    assert big.form == B.LINEAR_PAIRS and big.launches_per_run == 1
+    # pairs lay out the low halves of fp32 operands, and operands whose rows are not aligned
+    assert linear(8192, 8192, 4096, dtype="fp32").workspace_bytes >= 1024 + 2 * 8192 * 4096 * 4
+    assert linear(8192, 8192, 4097, dtype="bf16").workspace_bytes >= 1024 + 2 * 8192 * 4097 * 2
+    for dtype, eb in (("bf16", 2), ("fp32", 4)):
+        odd, even = linear(64, 64, 1001, dtype=dtype), linear(64, 64, 1001, dtype=dtype, ldx=1008, ldw=1008)
+        assert odd.form == even.form == B.LINEAR_TILES and (odd.launches_per_run, even.launches_per_run) == (2, 1)
+        assert odd.workspace_bytes >= 1024 + 128 * 1001 * eb and even.workspace_bytes == 1024
+    assert linear(1, 64, 1002, dtype="fp32").form == B.LINEAR_FEW
+    for M in (1, 2, 4, 5, 16, 17, 100, 1000, 5000):
         for N in (1, 128, 1000, 50000):
             for dtype in B.TYPES:
                 i = linear(M, N, 512, dtype=dtype)
-                per = 256 if i.pair else 128
-                assert i.items == -(-N // per) * -(-M // i.rows_per_item) and i.rows_per_item <= (128 if dtype == "fp32" else 256)
+                if i.form != B.LINEAR_FEW:
+                    assert i.features_per_item == (256 if i.form == B.LINEAR_PAIRS else 128)
+                    assert i.items == -(-N // i.features_per_item) * -(-M // i.rows_per_item) and i.rows_per_item <= 256
                 assert i.split in (1, 2, 4, 8)
 
 
