@@ -46,8 +46,8 @@ struct LinearParams {
 
 template <int TYPE, bool COPY>
 struct Roles {
-    // copier or converter warps; four copiers where the epilogue's sums need the registers
-    static constexpr int kAux = COPY ? (TYPE == MNN_TYPE_FP32 ? 4 : 8) : (TYPE == MNN_TYPE_FP32 ? 8 : 0);
+    // copier or converter warps; for fp32 as many as leave the epilogue 128 registers
+    static constexpr int kAux = TYPE == MNN_TYPE_FP32 ? 6 : COPY ? 8 : 0;
     static constexpr int kThreads = 64 + 32 * (kEpiWarps + kAux);
 };
 
@@ -467,7 +467,7 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         // leaves fewer than 16 warps per SM
         t.form = MNN_LINEAR_FEW;
         t.bm = s.M;
-        t.feats = s.N / 2 >= 16ll * num_sms ? 2 : 1;
+        t.feats = s.M > 2 || s.N / 2 >= 16ll * num_sms ? 2 : 1;
         t.items = (s.N + t.feats - 1) / t.feats;
         t.split = 1;
         while (t.split < 8 && t.items * t.split < 16ll * num_sms && (long long)s.K * eb >= 1024ll * t.split) t.split *= 2;
@@ -484,7 +484,7 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     const double operand_bytes = ((double)s.M + s.N) * s.K * eb;
     t.relay = strides;
     if (t.relay) {
-        t.ld_relay = ((long long)s.K * eb + 15) / 16 * 16 / eb;
+        t.ld_relay = kblocks * 128 / eb;             // whole lines: a row's 128 bytes then lie in one
         t.relay_bytes = (s.M + (long long)s.N) * t.ld_relay * eb;
     }
     const double tile_relay = t.relay ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
@@ -508,7 +508,7 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     // Pairs of SMs (linear_pair.cu): half the rows of x per CTA, so that the tensor core and not the delivery decides.  fp32 (as
     // two FP16 halves, three products) needs a pass over both operands first, as rows that are not aligned do.
     if (s.M < 192 || t.form == MNN_LINEAR_COPIED) return t;
-    const long long ld = ((long long)s.K + 7) / 8 * 8, blocks = ((long long)s.K + 63) / 64;
+    const long long blocks = ((long long)s.K + 63) / 64, ld = blocks * 64;
     const double relay = strides || f32 ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
     for (int bm = 256; bm >= 128; bm -= 32) {
         const long long items = ((s.N + 255) / 256) * (long long)((s.M + bm - 1) / bm), pairs = num_sms / 2;

@@ -90,18 +90,24 @@ struct LinearStore {
     }
 };
 
-// fp32: sums without a finite value are taken again, term by term (an infinity's low half is no number).
+// fp32: sums without a finite value are taken again, term by term (an infinity's low half is no number).  The loop is kept out of
+// line and behind one branch: inlined, the compiler ran all of it under predicates for every sum (28 us of 54 at K = 1024).
+static __device__ __noinline__ float retake_sum(const float* x, const float* w, int K)
+{
+    float t = 0.0f;
+    for (int k = 0; k < K; ++k) t = fmaf(x[k], w[k], t);
+    return t;
+}
 template <int NUM>
 __device__ __forceinline__ void retake_sums(float (&s)[NUM], int rows, long long m0, int n, const float* x, long long ldx, const float* w, long long ldw, int K)
 {
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < NUM; ++j) any = any || (j < rows && !isfinite(s[j]));
+    if (!any) return;
 #pragma unroll
     for (int j = 0; j < NUM; ++j)
-        if (j < rows && !isfinite(s[j])) {
-            const float *xr = x + (m0 + j) * ldx, *wr = w + (long long)n * ldw;
-            float t = 0.0f;
-            for (int k = 0; k < K; ++k) t = fmaf(xr[k], wr[k], t);
-            s[j] = t;
-        }
+        if (j < rows && !isfinite(s[j])) s[j] = retake_sum(x + (m0 + j) * ldx, w + (long long)n * ldw, K);
 }
 
 template <int TYPE>

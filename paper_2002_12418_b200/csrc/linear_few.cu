@@ -63,7 +63,7 @@ linear_few_kernel(FewParams p)
 {
     typedef typename Elem<TYPE>::T T;
     constexpr int NUM = Wide<TYPE>::kNum;
-    constexpr int STEP = !ALIGNED || ROWS * FEATS > 4 ? 2 : ROWS * FEATS == 1 ? 8 : 4;       // pieces of a row that a lane has in flight
+    constexpr int STEP = !ALIGNED || ROWS * FEATS > 4 ? 2 : 4;       // pieces of a row that a lane has in flight
     constexpr int EB = sizeof(T);
     __shared__ float part[kWarps][ROWS * FEATS];
     const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
@@ -90,7 +90,7 @@ linear_few_kernel(FewParams p)
     const char *xb = static_cast<const char*>(p.x), *wb = static_cast<const char*>(p.w);
     const char *xe = xb + ((p.M - 1) * p.ldx + p.K) * EB, *we = wb + ((p.N - 1) * p.ldw + p.K) * EB;
     auto w_piece = [&](const T* row, int i) -> uint4 {
-        if (ALIGNED) return __ldcs(reinterpret_cast<const uint4*>(row) + i);
+        if (ALIGNED) return __ldg(reinterpret_cast<const uint4*>(row) + i);
         return load_piece<EB>(reinterpret_cast<const char*>(row) + i * 16ll, 16, wb, we);
     };
     auto x_piece = [&](const T* row, int i) -> uint4 {

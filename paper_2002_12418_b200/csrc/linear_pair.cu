@@ -252,13 +252,17 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     }
                     const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * (uint32_t)kPairN;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        if (ch0 + c < ch1) {
-                            uint32_t v[16];
-                            ptx::tmem_ld16(taddr + (uint32_t)((ch0 + c) * 16), v);
+                    for (int c = 0; c < 8; c += 2)
+                        if (ch0 + c < ch1) {          // (an odd last chunk's partner is read too, and not used)
+                            uint32_t va[16], vb[16];
+                            ptx::tmem_ld16(taddr + (uint32_t)((ch0 + c) * 16), va);
+                            ptx::tmem_ld16(taddr + (uint32_t)(min(ch0 + c + 1, n_chunks - 1) * 16), vb);
                             ptx::tmem_ld_wait();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) sum[c][j] += __uint_as_float(v[j]);
+                            for (int j = 0; j < 16; ++j) {
+                                sum[c][j] += __uint_as_float(va[j]);
+                                sum[c + 1][j] += __uint_as_float(vb[j]);
+                            }
                         }
                     release_acc();
                 }

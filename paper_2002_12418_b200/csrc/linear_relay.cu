@@ -19,7 +19,7 @@ constexpr int kWarps = 8;
 
 struct RelayParams {
     LinearRelayed t[2];
-    int K, pieces;                   // 16-byte pieces of a row
+    int K;
     long long ld_out;                // elements
 };
 
@@ -38,24 +38,19 @@ linear_relay_kernel(RelayParams p)
         const char* const begin = static_cast<const char*>(t.src);
         const char* const end = begin + ((t.rows - 1) * t.ld + p.K) * EB;
         const char* const src = begin + row * t.ld * EB;
-        auto piece = [&](int i) { return load_piece<EB>(src + (long long)i * 16, min(16, p.K * EB - i * 16), begin, end); };
         if (HALVES) {
             uint32_t most = 0;
-#pragma unroll 4
-            for (int i = lane; i < p.pieces; i += 32) {
-                const uint4 v = piece(i);
+            for_pieces<EB>(src, p.K * EB, begin, end, lane, [&](int, const uint4& v) {
                 const uint32_t u[4] = {v.x & 0x7fffffffu, v.y & 0x7fffffffu, v.z & 0x7fffffffu, v.w & 0x7fffffffu};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = max(most, u[j] < 0x7f800000u ? u[j] : 0u);
-            }
+            });
             most = __reduce_max_sync(0xffffffffu, most);
             const int up = min(14 - ((int)(most >> 23) - 127), 127);                 // -113..127
             const float scale = __uint_as_float((uint32_t)(up + 127) << 23);
             __half* const hi = static_cast<__half*>(t.same) + row * p.ld_out;
             __half* const lo = static_cast<__half*>(t.low) + row * p.ld_out;
-#pragma unroll 4
-            for (int i = lane; i < p.pieces; i += 32) {
-                const uint4 v = piece(i);
+            for_pieces<EB>(src, p.K * EB, begin, end, lane, [&](int i, const uint4& v) {
                 const float f[4] = {__uint_as_float(v.x) * scale, __uint_as_float(v.y) * scale, __uint_as_float(v.z) * scale, __uint_as_float(v.w) * scale};
                 __half h[4], l[4];
 #pragma unroll
@@ -65,12 +60,11 @@ linear_relay_kernel(RelayParams p)
                 }
                 *reinterpret_cast<uint2*>(hi + i * 4) = *reinterpret_cast<const uint2*>(h);
                 *reinterpret_cast<uint2*>(lo + i * 4) = *reinterpret_cast<const uint2*>(l);
-            }
+            });
             if (lane == 0) t.up[row] = up;
         } else {
             uint4* const out = reinterpret_cast<uint4*>(static_cast<char*>(t.same) + row * p.ld_out * EB);
-#pragma unroll 4
-            for (int i = lane; i < p.pieces; i += 32) out[i] = piece(i);
+            for_pieces<EB>(src, p.K * EB, begin, end, lane, [&](int i, const uint4& v) { out[i] = v; });
         }
     }
 }
@@ -83,9 +77,8 @@ cudaError_t launch_linear_relay(const LinearRelayed& x, const LinearRelayed& w, 
     p.t[0] = x;
     p.t[1] = w;
     p.K = K;
-    p.pieces = (K * elem_bytes + 15) / 16;
     p.ld_out = ld_out;
-    const long long blocks = (x.rows + w.rows + kWarps - 1) / kWarps, most = 8ll * num_sms;
+    const long long blocks = (x.rows + w.rows + kWarps - 1) / kWarps, most = 16ll * num_sms;
     auto kern = elem_bytes == 2 ? linear_relay_kernel<2, false> : x.low ? linear_relay_kernel<4, true> : linear_relay_kernel<4, false>;
     return launch_overlapped(kern, dim3((unsigned)(blocks < most ? blocks : most)), dim3(32 * kWarps), 0, stream, p);
 }
