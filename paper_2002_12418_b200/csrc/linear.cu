@@ -48,6 +48,7 @@ template <int TYPE, bool COPY>
 struct Roles {
     // copier or converter warps; for fp32 as many as leave the epilogue 128 registers
     static constexpr int kAux = TYPE == MNN_TYPE_FP32 ? 6 : COPY ? 8 : 0;
+    static constexpr int kGroups = 3;            // of converter warps: each takes every third block, for the latency of a block
     static constexpr int kThreads = 64 + 32 * (kEpiWarps + kAux);
 };
 
@@ -76,14 +77,16 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t a_bytes = kTileF * 128, b_bytes = (uint32_t)p.bm * 128;
-    // stage: [A] x KB [B] x KB, for fp32 followed by [A low][B low]
+    // stage: [A] x KB [B] x KB, for fp32 followed by [B low][A low]: B and its low half lie together as one operand of 2 bm rows, so
+    // that hi*hi and hi*lo are one instruction and A is read twice and not three times.  The loop is bound by shared memory's
+    // 128 bytes a clock (64 rows of x: 56 KB read by the tensor core and 72 KB by copies and conversion, per block of K).
     const uint32_t raw_bytes = (a_bytes + b_bytes) * KB, stage_bytes = raw_bytes * (F32 ? 2 : 1), off_b = a_bytes * KB;
     volatile int* abortp = &abort_flag;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             ptx::mbar_init(ptx::smem_u32(&full_bar[s]), COPY ? kAux : 1);
-            ptx::mbar_init(ptx::smem_u32(&low_bar[s]), kAux ? kAux : 1);
+            ptx::mbar_init(ptx::smem_u32(&low_bar[s]), kAux ? kAux / Roles<TYPE, COPY>::kGroups : 1);
             ptx::mbar_init(ptx::smem_u32(&empty_bar[s]), 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -151,6 +154,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     } else if (warp == 1) {
         // instruction format: 2 = TF32, 1 = BF16, 0 = FP16
         const uint32_t idesc = ptx::mma_idesc(F32 ? 2 : TYPE == MNN_TYPE_BF16 ? 1 : 0, kTileF, p.bm);
+        const uint32_t idesc2 = ptx::mma_idesc(2, kTileF, 2 * p.bm);
         constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);       // 8-row groups 1024 bytes apart, 128-byte swizzle
         uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
         bool ok = true;
@@ -181,11 +185,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                             for (int ks = 0; ks < 4; ++ks) {
                                 const uint32_t a = a0 + h * (a_bytes >> 4) + ks * 2, b = b0 + h * (b_bytes >> 4) + ks * 2;
                                 const uint32_t go = h || ks ? 1u : accumulate;
-                                ptx::mma_lo<F32 ? 0 : 1>(d_main, a, b, kDescHi, idesc, go);
-                                if (F32) {
-                                    ptx::mma_lo<0>(d_cross, a + (raw_bytes >> 4), b, kDescHi, idesc, go);
-                                    ptx::mma_lo<0>(d_cross, a, b + (raw_bytes >> 4), kDescHi, idesc, 1u);
-                                }
+                                ptx::mma_lo<F32 ? 0 : 1>(d_main, a, b, kDescHi, F32 ? idesc2 : idesc, go);     // fp32: into d_cross too
+                                if (F32) ptx::mma_lo<0>(d_cross, a + ((raw_bytes + b_bytes) >> 4), b, kDescHi, idesc, 1u);
                             }
                         ptx::mma_commit(ptx::smem_u32(&empty_bar[stage]));
                     }
@@ -326,18 +327,18 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 uint8_t* const sbase = generic_base + stage * stage_bytes;
                 const int k0 = kb * kBlockElems + piece * (16 / EB);
                 const int valid = min(16, (p.K - k0) * EB);
-                auto rows_of = [&](const char* base, const char* end, long long ld, int row0, int total, int rows, uint8_t* tile) {
+                auto rows_of = [&](const char* base, const char* end, long long ld, int row0, int total, int rows, uint8_t* tile, uint32_t to_low) {
 #pragma unroll 4
                     for (int r = w * 4 + sub; r < rows; r += 4 * kAux) {
                         uint4 v = make_uint4(0, 0, 0, 0);
                         if (row0 + r < total && valid > 0) v = load_piece<EB>(base + ((long long)(row0 + r) * ld + k0) * EB, valid, base, end);
                         const uint32_t at = (uint32_t)r * 128u + (uint32_t)((piece ^ (r & 7)) << 4);
                         *reinterpret_cast<uint4*>(tile + at) = v;
-                        if (F32) *reinterpret_cast<float4*>(tile + raw_bytes + at) = low_half(make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)));
+                        if (F32) *reinterpret_cast<float4*>(tile + to_low + at) = low_half(make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)));
                     }
                 };
-                rows_of(wb, we, p.ldw, fb * kTileF, p.N, kTileF, sbase);
-                rows_of(xb, xe, p.ldx, mb * p.bm, p.M, p.bm, sbase + off_b);
+                rows_of(wb, we, p.ldw, fb * kTileF, p.N, kTileF, sbase, raw_bytes + b_bytes);
+                rows_of(xb, xe, p.ldx, mb * p.bm, p.M, p.bm, sbase + off_b, b_bytes);
                 fence_proxy_async_smem();                      // the tensor core reads these through the async proxy
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&full_bar[stage]));
@@ -349,28 +350,33 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
     } else if (F32) {
         // converters: the low halves of both tiles, in the same (swizzled) places
-        const int t = threadIdx.x - 32 * (2 + kEpiWarps);
+        constexpr int kPer = kAux / Roles<TYPE, COPY>::kGroups;          // warps of a group
+        const int w = warp - 2 - kEpiWarps, group = w / kPer, t = (w - group * kPer) * 32 + lane;
         uint32_t stage = 0, phase = 0;
+        int turn = 0;
         bool ok = true;
         uint8_t* const generic_base = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
         for (long long item = first_item; item < p.items && ok; item += item_step)
             for (int kb = kb0; kb < kb1; ++kb) {
-                int got = 1;
-                if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&full_bar[stage]), phase, abortp) ? 1 : 0;
-                got = __shfl_sync(0xffffffffu, got, 0);
-                if (!got) {
-                    if (lane == 0) failed(kErrAux);
-                    ok = false;
-                    break;
-                }
-                const float4* const raw = reinterpret_cast<const float4*>(generic_base + stage * stage_bytes);
-                float4* const low = reinterpret_cast<float4*>(generic_base + stage * stage_bytes + raw_bytes);
-                const int count = (int)(raw_bytes >> 4);
+                if (turn == group) {
+                    int got = 1;
+                    if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&full_bar[stage]), phase, abortp) ? 1 : 0;
+                    got = __shfl_sync(0xffffffffu, got, 0);
+                    if (!got) {
+                        if (lane == 0) failed(kErrAux);
+                        ok = false;
+                        break;
+                    }
+                    const float4* const raw = reinterpret_cast<const float4*>(generic_base + stage * stage_bytes);
+                    float4* const low = reinterpret_cast<float4*>(generic_base + stage * stage_bytes + raw_bytes);
+                    const int a_count = (int)(a_bytes >> 4), b_count = (int)(b_bytes >> 4), count = a_count + b_count;
 #pragma unroll 4
-                for (int i = t; i < count; i += 32 * kAux) low[i] = low_half(raw[i]);
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&low_bar[stage]));
+                    for (int i = t; i < count; i += 32 * kPer) low[i < a_count ? i + b_count : i - a_count] = low_half(raw[i]);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&low_bar[stage]));
+                }
+                if (++turn == Roles<TYPE, COPY>::kGroups) turn = 0;
                 if (++stage == (uint32_t)p.stages) {
                     stage = 0;
                     phase ^= 1u;
@@ -474,7 +480,7 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         return t;
     }
     // Estimated clocks of the tile kernel: waves of CTAs, each its share of K blocks at the slower of the tensor core (4096
-    // multiply-adds of 16 bits a clock; TF32 a third of that, three products) and the delivery of the tiles (about 48 bytes a clock
+    // multiply-adds of 16 bits a clock; fp32: shared memory) and the delivery of the tiles (about 48 bytes a clock
     // and SM by TMA, 3 by copier warps), plus start and end.  Rows whose strides TMA cannot copy are laid out anew first, at
     // about 20 bytes a clock and SM; where only a tensor's start is not aligned no workspace is kept for that, and copier warps
     // fetch it (64 x 4097 x 4096 BF16: 79 us by them).
@@ -493,8 +499,9 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         if (bm > 16 && bm / 2 >= s.M) break;
         const long long items = fblocks * ((s.M + bm - 1) / bm);
         for (int split = 1; split <= 8; split *= 2) {
-            if (split > 1 && (items * split > num_sms || kblocks < 2 * split)) break;
-            const double mma = f32 ? 9.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.form == MNN_LINEAR_COPIED ? 3.0 : 48.0);
+            // (clusters of eight: only as many as surely run at one time)
+            if (split > 1 && (items * split > num_sms || kblocks < 2 * split || (split == 8 && items > 8))) break;
+            const double mma = f32 ? 700.0 + 6.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.form == MNN_LINEAR_COPIED ? 3.0 : 48.0);
             const long long waves = (items * split + num_sms - 1) / num_sms;
             const double clocks = waves * ((kblocks + split - 1) / split * (mma > load ? mma : load)) + 1500.0 + 8.0 * bm + (split > 1 ? 1200.0 + 6.0 * bm : 0.0) + tile_relay;
             if (best == 0 || clocks < best) {
@@ -512,7 +519,7 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     const double relay = strides || f32 ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
     for (int bm = 256; bm >= 128; bm -= 32) {
         const long long items = ((s.N + 255) / 256) * (long long)((s.M + bm - 1) / bm), pairs = num_sms / 2;
-        const double clocks = (double)((items + pairs - 1) / pairs) * (blocks * (f32 ? 7.8 : 2.6) * bm + 1000.0) + 3500.0 + relay;
+        const double clocks = (double)((items + pairs - 1) / pairs) * (blocks * (f32 ? 11.0 : 2.6) * bm + (f32 ? 6000.0 : 1000.0)) + 3500.0 + relay;
         if (clocks < best) {
             best = clocks;
             t.form = MNN_LINEAR_PAIRS;
