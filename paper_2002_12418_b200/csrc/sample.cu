@@ -45,11 +45,9 @@ constexpr int kMaxScale = 45;
 constexpr int kMostBytes = 176 * 1024;   // of a row's logits in one CTA: the largest vocabulary in fp32 over eight CTAs, and a step of rounding up
 
 template <int TYPE> struct Logit { typedef float T; static constexpr int kVec = 4; };
-template <> struct Logit<MNN_TYPE_BF16> { typedef __nv_bfloat16 T; static constexpr int kVec = 8; };
 template <> struct Logit<MNN_TYPE_FP16> { typedef __half T; static constexpr int kVec = 8; };
 
 __device__ __forceinline__ float widen(float v) { return v; }
-__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float widen(__half v) { return __half2float(v); }
 
 // An integer that orders as the values do.
@@ -594,11 +592,11 @@ sample_kernel(SampleParams p)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     const float d = distance(l[j]);
-                    const u64 here = l[j] >= floor_l ? w[j] : 0;     // (a NaN's weight is none)
+                    const bool counts = l[j] >= floor_l && l[j] > -INFINITY;
+                    const u64 here = counts ? w[j] : 0;
                     sum += here;
-                    if (d < d0) {
-                        sum_above += here;
-                    } else if (d < d1 && here) {
+                    sum_above += d < d0 ? here : 0;
+                    if (counts && d >= d0 && d < d1) {
                         const int b = fine(d);
                         atomicAdd(&sh.count[b], 1u);
                         add_mass(b, here);
@@ -639,7 +637,7 @@ sample_kernel(SampleParams p)
                 const float b1 = bin < kBins - 1 ? __uint_as_float(bits0 + ((uint32_t)(bin + 1) << 9)) : d1;
                 narrow(true, target, [&](float l) {
                     const float d = distance(l);
-                    return d >= b0 && d < b1 && weight(l) != 0;
+                    return l >= floor_l && d >= b0 && d < b1;
                 });
             } else {
                 sync_row();                                          // (the histograms are zero again for all)
@@ -836,6 +834,616 @@ sample_kernel(SampleParams p)
     sync_row();                                                      // nobody leaves while its sums are being read
 }
 
+// ---- BF16 rows: by values
+//
+// BF16 logits have few values: below a largest logit of 10, 1568 down to 2^-9.  A bin per value makes counts enough: its mass is
+// the count times one weight, so weights are evaluated once per value and not once per element (the row's passes were bound by
+// that evaluation, some 75 instructions), the bin that a border crosses is the border, and a CTA's kept mass follows from its own
+// counts.  Only the CTA whose part of the row holds the drawn token looks at its elements again.
+// The bins count values down from the largest logit by their bits.  What lies within 2^-9 of zero shares one bin, and so does what
+// is more than 4094 values below the largest: in these two, weights are summed element by element, and a border that falls there
+// is found by halving the range of keys.
+constexpr int kValues = 4096;
+constexpr int kNearZero = 0x3b00;        // the bits of 2^-9
+
+struct SharedValues {
+    float warp_max[kMaxWarps];
+    float max;                       // of this CTA
+    uint32_t special[2][3];          // planes of the masses of the two shared bins, of this CTA
+    u64 share_mass;
+    uint32_t share_count;
+    u64 scan_mass[kMaxWarps];
+    uint32_t scan_count[kMaxWarps];
+    u64 warp_mass[kMaxWarps];
+    uint32_t warp_count[kMaxWarps];
+    u64 cta_mass;
+    uint32_t cta_count;
+    uint32_t key_min, key_max;       // of this CTA
+    u64 half_mass;                   // of this CTA, while a range is halved
+    uint32_t half_count;
+    u64 found_mass, found_whole;
+    uint32_t found_count, found_equal;
+    int found_bin;
+    u64 ties_kept[kMaxWarps];
+};
+
+__global__ void __launch_bounds__(32 * kMaxWarps, 2)
+sample_values_kernel(SampleParams p)
+{
+    typedef __nv_bfloat16 T;
+    constexpr int VEC = 8;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    __shared__ SharedValues sh;
+
+    const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31, n_threads = blockDim.x;
+    const uint32_t rank = ptx::cluster_ctarank();
+    uint32_t n_ctas;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
+    const int row = blockIdx.x / n_ctas;
+    const int share = kValues / (int)n_ctas;                         // bins that this CTA sums over the cluster
+    // the row's part, its counts, and running sums through this CTA's share of the bins
+    uint32_t* const held = reinterpret_cast<uint32_t*>(smem_raw);    // two logits each
+    uint32_t* const count = reinterpret_cast<uint32_t*>(smem_raw + (size_t)p.run * p.n_warps * 2);
+    u64* const run_mass = reinterpret_cast<u64*>(count + kValues);
+    uint32_t* const run_count = reinterpret_cast<uint32_t*>(run_mass + share);
+    auto sync_row = [&]() {
+        if (n_ctas > 1) ptx::cluster_sync_all();
+        else __syncthreads();
+    };
+
+    ptx::grid_launch_dependents();
+    for (int i = threadIdx.x; i < kValues / 4; i += n_threads) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x < 6) sh.special[threadIdx.x / 3][threadIdx.x % 3] = 0;
+    ptx::grid_dependency_wait();
+
+    // ---- load (positions and runs as above)
+    const int warp0 = warp * p.run, cta0 = (int)rank * p.run * p.n_warps;
+    const T* const row_ptr = static_cast<const T*>(p.a.logits) + (long long)row * p.ld;
+    const int shift = (int)((reinterpret_cast<uintptr_t>(row_ptr) & 15u) / sizeof(T));
+    float top = -INFINITY;
+    {
+        const unsigned short* const base = reinterpret_cast<const unsigned short*>(row_ptr) - shift;
+        const int first = shift, last = shift + p.vocab;
+#pragma unroll 4
+        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+            const int at = cta0 + warp0 + i;
+            uint4 q;
+            if (at >= first && at + VEC <= last) {
+                q = __ldg(reinterpret_cast<const uint4*>(base + at));
+            } else {
+                uint32_t u[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t a = at + 2 * j >= first && at + 2 * j < last ? base[at + 2 * j] : 0xff80u;
+                    const uint32_t b = at + 2 * j + 1 >= first && at + 2 * j + 1 < last ? base[at + 2 * j + 1] : 0xff80u;
+                    u[j] = a | (b << 16);
+                }
+                q = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+            *reinterpret_cast<uint4*>(held + ((warp0 + i) >> 1)) = q;
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xffff0000u)));
+        }
+    }
+    const float temperature = p.a.temperature ? p.a.temperature[row] : 1.0f;
+    const int top_k = p.a.top_k ? p.a.top_k[row] : 0;
+    const float top_p = p.a.top_p ? p.a.top_p[row] : 1.0f;
+    const float min_p = p.a.min_p ? p.a.min_p[row] : 0.0f;
+    const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
+    const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) sh.warp_max[warp] = top;
+    __syncthreads();
+    if (warp == 0) {
+        top = lane < p.n_warps ? sh.warp_max[lane] : -INFINITY;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (lane == 0) sh.max = top;
+    }
+    sync_row();
+    float m = -INFINITY;
+    for (uint32_t r = 0; r < n_ctas; ++r) m = fmaxf(m, __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(&sh.max), r)));
+    m += 0.0f;                                                       // (one zero)
+    const bool some = m > -INFINITY;
+
+    // ---- weights, as above
+    const bool m_inf = m == INFINITY;
+    const double slope = one ? 0.0 : 1.4426950408889634074 / (double)temperature;         // log2(e) / T
+    const float floor_l = m_inf || one ? m : m - (float)(p.scale_log2 + 3) * 0.6931472f * temperature;
+    const double m_wide = (double)m;
+    const u64 unit = 1ull << p.scale_log2;
+    auto weight = [&](float l) -> u64 {
+        const double d = l == m ? 0.0 : __dsub_rn((double)fmaxf(l, floor_l), m_wide);
+        const u64 w = exp2_units(d, slope, p.scale_log2);
+        return l < floor_l ? 0 : w;
+    };
+    auto key = [&](float l) { return key_of(l + 0.0f); };
+
+    // ---- bins: rank_of counts values up from -largest through the shared one at 0
+    auto rank_of = [](float l) {
+        const int bits = (int)(__float_as_uint(l) >> 16), a = max((bits & 0x7fff) - kNearZero, 0);
+        return bits & 0x8000 ? -a : a;
+    };
+    const int rank_m = rank_of(m), zero_bin = min(rank_m, kValues - 1);
+    // (a largest logit below the shared values has no bin for them; its own rank is negative then)
+    auto bin_of = [&](float l) { return min(rank_m - rank_of(l), kValues - 1); };
+    auto is_shared = [&](int b) { return b == zero_bin || b == kValues - 1; };
+    auto value_of_bin = [&](int b) {                                 // of a bin that holds one value
+        const int r = rank_m - b;
+        return __uint_as_float((uint32_t)(r > 0 ? r + kNearZero : 0x8000 | (kNearZero - r)) << 16);
+    };
+    auto for_each = [&](auto&& f) {
+        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+            const uint4 q = *reinterpret_cast<const uint4*>(held + ((warp0 + i) >> 1));
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f(__uint_as_float(u[j] << 16));
+                f(__uint_as_float(u[j] & 0xffff0000u));
+            }
+        }
+    };
+    if (some)
+        for_each([&](float l) {
+            if (l > -INFINITY) {
+                const int b = bin_of(l);
+                atomicAdd(&count[b], 1u);
+                if (is_shared(b) && l >= floor_l) {                  // rare
+                    const u64 w = weight(l);
+                    const int s = b == kValues - 1 ? 1 : 0;
+                    atomicAdd(&sh.special[s][0], (uint32_t)w & 0x7fffu);
+                    atomicAdd(&sh.special[s][1], (uint32_t)(w >> 15) & 0x7fffu);
+                    atomicAdd(&sh.special[s][2], (uint32_t)(w >> 30));
+                }
+            }
+        });
+    auto special_mass = [&](int b, uint32_t r) {
+        const uint32_t* const s = sh.special[b == kValues - 1 ? 1 : 0];
+        return (u64)ld_cluster(s, r) + ((u64)ld_cluster(s + 1, r) << 15) + ((u64)ld_cluster(s + 2, r) << 30);
+    };
+
+    u64 above_mass = 0;
+    uint32_t above_count = 0, bin_count = 0;
+    int bin = -1;
+    auto merge = [&](bool masses) {
+        sync_row();
+        const int b0 = (int)rank * share, per = (share + n_threads - 1) / n_threads;
+        u64 sum_m = 0;
+        uint32_t sum_c = 0;
+        for (int j = 0; j < per; ++j) {
+            const int at = threadIdx.x * per + j, b = b0 + at;
+            if (at < share) {
+                uint32_t c = 0;
+                for (uint32_t r = 0; r < n_ctas; ++r) c += ld_cluster(&count[b], r);
+                if (masses && c) {
+                    if (is_shared(b)) {
+                        for (uint32_t r = 0; r < n_ctas; ++r) sum_m += special_mass(b, r);
+                    } else {
+                        sum_m += c * weight(value_of_bin(b));
+                    }
+                }
+                sum_c += c;
+                run_mass[at] = sum_m;                                // (running within this thread; the rest is added below)
+                run_count[at] = sum_c;
+            }
+        }
+        const u64 scan_m = masses ? warp_scan(sum_m, lane) : 0;
+        const uint32_t scan_c = warp_scan(sum_c, lane);
+        if (lane == 31) {
+            sh.scan_mass[warp] = scan_m;
+            sh.scan_count[warp] = scan_c;
+        }
+        __syncthreads();
+        u64 base_m = scan_m - sum_m;
+        uint32_t base_c = scan_c - sum_c;
+        for (int i = 0; i < warp; ++i) {
+            base_m += sh.scan_mass[i];
+            base_c += sh.scan_count[i];
+        }
+        for (int j = 0; j < per; ++j) {
+            const int at = threadIdx.x * per + j;
+            if (at < share) {
+                run_mass[at] += base_m;
+                run_count[at] += base_c;
+            }
+        }
+        if (threadIdx.x == n_threads - 1) {
+            sh.share_mass = base_m + sum_m;
+            sh.share_count = base_c + sum_c;
+        }
+        sync_row();
+    };
+    // The first bin at which the running count (or mass) reaches `target`: found by one warp of each CTA, told to all.
+    auto cross = [&](bool use_mass, u64 target) {
+        if (warp == 0) {
+            u64 base_m = 0;
+            uint32_t base_c = 0, here = 0;
+            int found = -1;
+            for (uint32_t r = 0; r < n_ctas && found < 0; ++r) {
+                const u64 sm = ld_cluster(&sh.share_mass, r);
+                const uint32_t sc = ld_cluster(&sh.share_count, r);
+                if (use_mass ? base_m + sm >= target : (u64)base_c + sc >= target) {
+                    // 32 places through the share, then the bins between two of them
+                    const int step = share >> 5;
+                    int lo = 0;
+                    for (int wide = step; found < 0; wide = 1) {
+                        const int at = wide > 1 ? (lane + 1) * wide - 1 : lo + lane;
+                        const u64 rm = at < share ? ld_cluster(&run_mass[at], r) : 0;
+                        const uint32_t rc = at < share ? ld_cluster(&run_count[at], r) : 0;
+                        const unsigned hit = __ballot_sync(0xffffffffu, at < share && (use_mass ? base_m + rm >= target : (u64)base_c + rc >= target));
+                        const int src = hit ? __ffs(hit) - 1 : 31;
+                        if (wide > 1) {
+                            lo = src * wide;
+                        } else if (hit || lo + 32 >= share) {
+                            found = lo + src;
+                        } else {
+                            lo += 32;
+                        }
+                    }
+                    const u64 bm = found ? ld_cluster(&run_mass[found - 1], r) : 0;
+                    const uint32_t bc = found ? ld_cluster(&run_count[found - 1], r) : 0;
+                    here = ld_cluster(&run_count[found], r) - bc;
+                    base_m += bm;
+                    base_c += bc;
+                    found += (int)r * share;
+                } else {
+                    base_m += sm;
+                    base_c += sc;
+                }
+            }
+            if (lane == 0) {
+                sh.found_bin = found;
+                sh.found_mass = base_m;
+                sh.found_count = base_c;
+                sh.found_equal = here;
+            }
+        }
+        __syncthreads();
+        bin = sh.found_bin;
+        above_mass = sh.found_mass;
+        above_count = sh.found_count;
+        bin_count = sh.found_equal;
+        __syncthreads();
+    };
+    uint32_t border_key = 0, border_equal = 0;
+    // The border in the crossing bin.
+    auto narrow = [&](bool use_mass, u64 target) {
+        if (!is_shared(bin)) {
+            border_key = key(value_of_bin(bin));
+            border_equal = bin_count;
+            return;
+        }
+        // by halving the range of its keys: the largest at which the elements from it on reach the target
+        const int b = bin;
+        uint32_t mn = 0xffffffffu, mx = 0;
+        if (threadIdx.x == 0) {
+            sh.key_min = mn;
+            sh.key_max = mx;
+        }
+        __syncthreads();
+        for_each([&](float l) {
+            if (l > -INFINITY && bin_of(l) == b) {
+                mn = min(mn, key(l));
+                mx = max(mx, key(l));
+            }
+        });
+        mn = __reduce_min_sync(0xffffffffu, mn);
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        if (lane == 0) {
+            atomicMin(&sh.key_min, mn);
+            atomicMax(&sh.key_max, mx);
+        }
+        sync_row();
+        uint32_t lo = 0xffffffffu, hi = 0;
+        for (uint32_t r = 0; r < n_ctas; ++r) {
+            lo = min(lo, ld_cluster(&sh.key_min, r));
+            hi = max(hi, ld_cluster(&sh.key_max, r));
+        }
+        // mass and number of the bin's elements with a key of at least k
+        u64 mass_k = 0;
+        uint32_t count_k = 0;
+        auto from_key = [&](uint32_t k) {
+            u64 s = 0;
+            uint32_t c = 0;
+            for_each([&](float l) {
+                if (l > -INFINITY && bin_of(l) == b && key(l) >= k) {
+                    ++c;
+                    if (use_mass) s += weight(l);
+                }
+            });
+            s = warp_sum(s);
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (lane == 0) {
+                sh.warp_mass[warp] = s;
+                sh.warp_count[warp] = c;
+            }
+            __syncthreads();
+            if (warp == 0) {
+                const u64 a = warp_sum(lane < p.n_warps ? sh.warp_mass[lane] : 0);
+                const uint32_t n = __reduce_add_sync(0xffffffffu, lane < p.n_warps ? sh.warp_count[lane] : 0u);
+                if (lane == 0) {
+                    sh.half_mass = a;
+                    sh.half_count = n;
+                }
+            }
+            sync_row();
+            mass_k = 0;
+            count_k = 0;
+            for (uint32_t r = 0; r < n_ctas; ++r) {
+                mass_k += ld_cluster(&sh.half_mass, r);
+                count_k += ld_cluster(&sh.half_count, r);
+            }
+            sync_row();
+        };
+        for (int step = 0; step < 32 && lo < hi; ++step) {
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            from_key(mid);
+            if (use_mass ? above_mass + mass_k >= target : (u64)above_count + count_k >= target) lo = mid;
+            else hi = mid - 1;
+        }
+        from_key(lo);
+        const uint32_t with = count_k;
+        from_key(lo + 1);                                            // (a key is never the last integer: that would be a NaN)
+        above_mass += mass_k;
+        above_count += count_k;
+        border_equal = with - count_k;
+        border_key = lo;
+    };
+
+    // ---- the border: everything above its value is kept, and the first `ties` equal to it
+    bool cut = some && one;
+    u64 ties = 1;
+    if (cut) border_key = key(m);
+    if (some && (by_count || by_mass)) {
+        merge(by_mass);
+        if (by_count) {
+            cross(false, (u64)top_k);
+            if (bin >= 0) {                                          // else fewer candidates than k: all are kept
+                narrow(false, (u64)top_k);
+                ties = (u64)top_k - above_count;
+                cut = true;
+            }
+        }
+        if (by_mass) {
+            u64 whole = 0;
+            if (cut && !is_shared(bin)) {
+                whole = above_mass + ties * weight(value_of_key(border_key));
+            } else if (cut) {                                        // the masses above a border in a shared bin were not summed
+                const float from = value_of_key(border_key);
+                u64 s = 0;
+                for_each([&](float l) {
+                    if (l > from) s += weight(l);
+                });
+                s = warp_sum(s);
+                if (lane == 0) sh.warp_mass[warp] = s;
+                __syncthreads();
+                if (warp == 0) {
+                    const u64 a = warp_sum(lane < p.n_warps ? sh.warp_mass[lane] : 0);
+                    if (lane == 0) sh.half_mass = a;
+                }
+                sync_row();
+                for (uint32_t r = 0; r < n_ctas; ++r) whole += ld_cluster(&sh.half_mass, r);
+                sync_row();
+                whole += ties * weight(from);
+            } else {
+                for (uint32_t r = 0; r < n_ctas; ++r) whole += ld_cluster(&sh.share_mass, r);
+            }
+            // kept while the mass before < p * whole: up to where the running mass reaches ceil(p * whole)
+            const u64 target = max(1ull, min((u64)ceil((double)fmaxf(top_p, 0.0f) * (double)whole), whole));
+            cross(true, target);
+            narrow(true, target);
+            const u64 w = weight(value_of_key(border_key));
+            ties = (target - above_mass + w - 1) / w;
+            cut = true;
+        }
+    } else {
+        __syncthreads();                                             // (the counts are read below)
+    }
+
+    // ---- draw: what each CTA keeps, by its counts; then, in the CTA that holds the token, its runs and elements
+    const float border_value = cut ? value_of_key(border_key) : -INFINITY;
+    const u64 least = min_p > 0.0f ? max(1ull, (u64)ceil((double)fminf(min_p, 1.0f) * (double)unit)) : 0;
+    const u64 border_w = cut ? weight(border_value) : 0;
+    const bool equals_count = cut && border_w >= least;
+    const float from = fmaxf(border_value, floor_l);                 // nothing below weighs anything
+    auto kept_above = [&](float l) -> u64 {
+        const u64 w = weight(l);
+        return w >= least ? w : 0;
+    };
+    u64 mass = 0;
+    uint32_t equals = 0;
+    if (some) {
+        const int last = cut ? bin_of(border_value) : kValues - 1;   // the border's bin
+        for (int b = threadIdx.x; b <= last; b += n_threads) {
+            const uint32_t c = count[b];
+            if (!c) continue;
+            if (!is_shared(b)) {
+                const float l = value_of_bin(b);
+                if (l > border_value) {
+                    if (l >= from) mass += c * kept_above(l);
+                } else if (equals_count && l == border_value) {
+                    equals += c;
+                }
+            } else if (least == 0 && b != last) {                    // all of a shared bin
+                mass += special_mass(b, rank);
+            }
+        }
+        // a shared bin of which the border or min-p may keep a part: by elements
+        const bool parts = (count[zero_bin < 0 ? kValues - 1 : zero_bin] && zero_bin >= 0 && zero_bin <= last && (least > 0 || zero_bin == last)) ||
+                           (last == kValues - 1 && count[kValues - 1]);
+        if (parts)
+            for_each([&](float l) {
+                if (l > -INFINITY) {
+                    const int b = bin_of(l);
+                    if (is_shared(b) && (least > 0 || b == last)) {
+                        if (l > border_value) {
+                            if (l >= from) mass += kept_above(l);
+                        } else if (equals_count && l == border_value) {
+                            ++equals;
+                        }
+                    }
+                }
+            });
+    }
+    mass = warp_sum(mass);
+    equals = __reduce_add_sync(0xffffffffu, equals);
+    if (lane == 0) {
+        sh.warp_mass[warp] = mass;
+        sh.warp_count[warp] = equals;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const u64 a = warp_sum(lane < p.n_warps ? sh.warp_mass[lane] : 0);
+        const uint32_t n = __reduce_add_sync(0xffffffffu, lane < p.n_warps ? sh.warp_count[lane] : 0u);
+        if (lane == 0) {
+            sh.cta_mass = a;
+            sh.cta_count = n;
+        }
+    }
+    sync_row();
+    // every warp: the CTAs' sums, with as many equals as still count
+    const u64 c_m = lane < (int)n_ctas ? ld_cluster(&sh.cta_mass, (uint32_t)lane) : 0;
+    const u64 c_c = lane < (int)n_ctas ? ld_cluster(&sh.cta_count, (uint32_t)lane) : 0;
+    const u64 c_seen = warp_scan(c_c, lane) - c_c;
+    const u64 c_v = c_m + (c_seen < ties ? min(c_c, ties - c_seen) : 0) * border_w;
+    const u64 c_incl = warp_scan(c_v, lane);
+    const u64 total = __shfl_sync(0xffffffffu, c_incl, 31);
+    const u64 seen0 = __shfl_sync(0xffffffffu, c_seen, (int)rank), before0 = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank), mine = __shfl_sync(0xffffffffu, c_v, (int)rank);
+    const double whole_kept = (double)total;
+    auto share_of = [&](float l) {                                   // weight / kept mass
+        const double w = l == m ? 1.0 : m_inf ? 0.0 : exp2(((double)l - m_wide) * slope);
+        return (float)(w * (double)unit / whole_kept);
+    };
+    u64 target = 0;
+    bool holds = false;
+    if (total == 0) {                                                // no candidate
+        if (rank == 0 && threadIdx.x == 0) {
+            p.a.token[row] = -1;
+            if (p.a.prob) p.a.prob[row] = 0.0f;
+        }
+    } else {
+        const float u_row = p.a.u[row];
+        const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;         // (a NaN counts as 0)
+        target = min((u64)((double)u * whole_kept), total - 1);
+        holds = target >= before0 && target < before0 + mine;        // this CTA's part holds the token
+    }
+    if (holds || p.a.probs) {
+        // this CTA's runs: masses above the border, and equals
+        u64 run_m = 0;
+        uint32_t run_c = 0;
+        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+            const uint4 q = *reinterpret_cast<const uint4*>(held + ((warp0 + i) >> 1));
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float l = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+                any = any || (l >= from && l > border_value);
+                run_c += equals_count && l == border_value ? 1u : 0u;
+            }
+            if (any) {
+                u64 w[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[j] = kept_above(__uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16));
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float l = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+                    run_m += l >= from && l > border_value ? w[j] : 0;
+                }
+            }
+        }
+        run_m = warp_sum(run_m);
+        run_c = __reduce_add_sync(0xffffffffu, run_c);
+        __syncthreads();                                             // (warp 0 has read the sums above)
+        if (lane == 0) {
+            sh.warp_mass[warp] = run_m;
+            sh.warp_count[warp] = run_c;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            run_m = lane < p.n_warps ? sh.warp_mass[lane] : 0;
+            const u64 rc = lane < p.n_warps ? sh.warp_count[lane] : 0;
+            const u64 seen = seen0 + warp_scan(rc, lane) - rc;
+            const u64 ties_run = seen < ties ? min(rc, ties - seen) : 0;
+            const u64 v = run_m + ties_run * border_w;
+            const u64 before = before0 + warp_scan(v, lane) - v;
+            if (lane < p.n_warps) sh.ties_kept[lane] = ties_run;
+            const unsigned owner = __ballot_sync(0xffffffffu, holds && target >= before && target < before + v);
+            if (owner) {
+                const int src = __ffs(owner) - 1, run0 = src * p.run;
+                u64 left = target - __shfl_sync(0xffffffffu, before, src), ties_left = __shfl_sync(0xffffffffu, ties_run, src);
+                for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+                    const uint4 q = *reinterpret_cast<const uint4*>(held + ((run0 + i) >> 1));
+                    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+                    float l[VEC];
+                    uint32_t eq = 0;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        l[j] = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+                        eq += equals_count && l[j] == border_value ? 1u : 0u;
+                    }
+                    const uint32_t eq_incl = warp_scan(eq, lane);
+                    u64 t = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;       // this lane's equals that still count
+                    u64 w[VEC], sum = 0;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        if (!(l[j] > border_value)) {
+                            const bool e = equals_count && l[j] == border_value && t > 0;
+                            w[j] = e ? border_w : 0;
+                            t -= e ? 1 : 0;
+                        }
+                        sum += w[j];
+                    }
+                    const u64 incl = warp_scan(sum, lane);
+                    const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
+                    if (hit) {
+                        if (lane == __ffs(hit) - 1) {
+                            u64 rest = left - (incl - sum);
+                            int at = -1;
+                            float drawn = 0.0f;
+#pragma unroll
+                            for (int j = 0; j < VEC; ++j) {
+                                if (at < 0 && rest < w[j]) {
+                                    at = j;
+                                    drawn = l[j];
+                                }
+                                rest -= w[j];
+                            }
+                            p.a.token[row] = cta0 + run0 + i + at - shift;
+                            if (p.a.prob) p.a.prob[row] = share_of(drawn);
+                        }
+                        break;
+                    }
+                    left -= __shfl_sync(0xffffffffu, incl, 31);
+                    const uint32_t eq_all = __shfl_sync(0xffffffffu, eq_incl, 31);
+                    ties_left = ties_left > eq_all ? ties_left - eq_all : 0;
+                }
+            }
+        }
+    }
+    if (p.a.probs) {                                                 // the whole filtered distribution
+        __syncthreads();
+        float* const out = p.a.probs + (long long)row * p.ld_probs;
+        u64 ties_left = sh.ties_kept[warp];
+        for (int i = lane; i < p.run; i += 32) {
+            const int at = cta0 + warp0 + i - shift;
+            const uint32_t pair = held[(warp0 + i) >> 1];
+            const float l = __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16);
+            const bool eq = equals_count && l == border_value;
+            const unsigned eqs = __ballot_sync(0xffffffffu, eq);
+            const bool keep = l > border_value ? (least == 0 || weight(l) >= least) : eq && (u64)__popc(eqs & ((1u << lane) - 1u)) < ties_left;
+            if (at >= 0 && at < p.vocab) out[at] = keep && total ? share_of(l) : 0.0f;
+            const u64 n = (u64)__popc(eqs);
+            ties_left = ties_left > n ? ties_left - n : 0;
+        }
+    }
+    sync_row();                                                      // nobody leaves while its sums are being read
+}
+
 template <int TYPE>
 cudaError_t run_sample(const SampleShape& s, const SampleTiling& t, const SampleParams& p, cudaStream_t stream)
 {
@@ -844,6 +1452,15 @@ cudaError_t run_sample(const SampleShape& s, const SampleTiling& t, const Sample
     cudaError_t e = allow_smem_once(reinterpret_cast<const void*>(sample_kernel<TYPE>), kMostBytes, &done);
     if (e != cudaSuccess) return e;
     return launch_cluster(t.ctas, sample_kernel<TYPE>, dim3((unsigned)(s.rows * t.ctas)), dim3(32 * t.warps), (size_t)bytes, stream, p);
+}
+
+cudaError_t run_values(const SampleShape& s, const SampleTiling& t, const SampleParams& p, cudaStream_t stream)
+{
+    static unsigned long long done = 0;
+    const int bytes = t.run * t.warps * 2 + kValues * 4 + kValues / t.ctas * 12;
+    cudaError_t e = allow_smem_once(reinterpret_cast<const void*>(sample_values_kernel), kMostBytes, &done);
+    if (e != cudaSuccess) return e;
+    return launch_cluster(t.ctas, sample_values_kernel, dim3((unsigned)(s.rows * t.ctas)), dim3(32 * t.warps), (size_t)bytes, stream, p);
 }
 
 }  // namespace
@@ -878,7 +1495,7 @@ cudaError_t launch_sample(const SampleShape& s, const SampleTiling& t, const Sam
     p.a = a;
     switch (s.type) {
         case MNN_TYPE_FP32: return run_sample<MNN_TYPE_FP32>(s, t, p, stream);
-        case MNN_TYPE_BF16: return run_sample<MNN_TYPE_BF16>(s, t, p, stream);
+        case MNN_TYPE_BF16: return run_values(s, t, p, stream);
         default: return run_sample<MNN_TYPE_FP16>(s, t, p, stream);
     }
 }

@@ -138,14 +138,36 @@ def test_edges_of_the_parameters():
     check(l, u, temperature=t, top_k=k, top_p=p, min_p=q)
 
 
-def test_wide_and_narrow_rows():
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [5000, 40001])
+def test_wide_and_narrow_rows(vocab, dtype):
     import torch
     for scale in (1e-6, 1e-3, 30.0, 1e4, 1e30):
-        l, u, g = make(torch, 10, 8, 5000, "fp32", scale=scale)
+        l, u, g = make(torch, 10, 8, vocab, dtype, scale=scale)
+        l = torch.where(torch.isinf(l), torch.finfo(l.dtype).max * torch.sign(l), l)
         p = torch.rand(8, generator=g, device="cuda")
         k = torch.randint(1, 3000, (8,), generator=g, device="cuda", dtype=torch.int32)
+        t = torch.full((8,), scale, device="cuda")
         check(l, u, top_p=p)
         check(l, u, top_k=k, top_p=p)
+        check(l, u, temperature=t, top_k=k, top_p=p, min_p=p * 0.01)
+        check(l, u, temperature=t, min_p=p * 0.1)
+
+
+# rows that lie around zero, wholly below it, and borders among the smallest values
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_rows_around_zero(dtype):
+    import torch
+    l, u, g = make(torch, 12, 10, 6000, dtype, scale=1.0)
+    l[0:2] -= 20.0
+    l[2:4] = -l[2:4].abs()
+    l[4:6] *= 1e-3
+    l[6:8] = torch.where(l[6:8].abs() < 1.0, l[6:8] * 1e-4, -l[6:8].abs())
+    l[8:10] = torch.where(l[8:10] > 2.0, l[8:10], l[8:10] * 1e-3)
+    p = torch.rand(10, generator=g, device="cuda")
+    k = torch.randint(1, 5000, (10,), generator=g, device="cuda", dtype=torch.int32)
+    for given in ({}, dict(top_k=k), dict(top_p=p), dict(top_k=k, top_p=p), dict(min_p=p), dict(top_p=p, min_p=p), dict(temperature=p * 1e-3, top_p=p)):
+        check(l, u, **given)
 
 
 # the draws follow the distribution: 20000 equal rows, the frequency of each token within 6 standard deviations
