@@ -71,6 +71,14 @@ __device__ __forceinline__ u64 ld_cluster(const u64* mine, uint32_t rank)
     return v;
 }
 
+// A value that was read from another CTA's shared memory has to be here before this thread arrives at the barrier behind which that
+// memory is written again or its CTA is gone; a use of it behind the barrier alone does not see to that (a first build read from
+// CTAs that had left).  So it decides a branch with a store that is never taken: the largest integer is no mass and no key.
+__device__ __forceinline__ void landed(u64 v, uint32_t* never)
+{
+    if (v == ~0ull) *reinterpret_cast<volatile uint32_t*>(never) = 1;
+}
+
 __device__ __forceinline__ u64 warp_sum(u64 v)
 {
 #pragma unroll
@@ -135,6 +143,7 @@ struct Shared {
     uint32_t all[kGather];           // of the cluster's
     u64 all_mass[kGather];
     // what one warp found, for all
+    uint32_t never;
     u64 found_mass, found_whole;
     uint32_t found_count, found_key, found_equal;
     int found_bin;
@@ -168,6 +177,7 @@ sample_kernel(SampleParams p)
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
     const int row = blockIdx.x / n_ctas;
     auto sync_row = [&]() {
+        __syncwarp();                                                // (the cluster's barrier takes whole warps)
         if (n_ctas > 1) ptx::cluster_sync_all();
         else __syncthreads();
     };
@@ -484,6 +494,7 @@ sample_kernel(SampleParams p)
                 lo = min(lo, ld_cluster(&sh.key_min, r));
                 hi = max(hi, ld_cluster(&sh.key_max, r));
             }
+            landed((u64)lo << 32 | hi, &sh.never);
             sync_row();
         };
         range(in);
@@ -737,6 +748,7 @@ sample_kernel(SampleParams p)
         const double w = l == m ? 1.0 : m_inf ? 0.0 : exp2(((double)l - m_wide) * slope);
         return (float)(w * (double)unit / whole);
     };
+    u64 total = 0, before0 = 0, seen0 = 0;
     if (warp == 0) {
         // the CTAs' sums, with as many equals as still count
         const u64 c_m = lane < (int)n_ctas ? ld_cluster(&sh.cta_mass, (uint32_t)lane) : 0;
@@ -744,12 +756,18 @@ sample_kernel(SampleParams p)
         const u64 cta_seen = warp_scan(c_c, lane) - c_c;
         const u64 c_v = c_m + (cta_seen < ties ? min(c_c, ties - cta_seen) : 0) * border_w;
         const u64 c_incl = warp_scan(c_v, lane);
-        const u64 total = __shfl_sync(0xffffffffu, c_incl, 31);
-        // and this CTA's runs
-        const u64 seen = __shfl_sync(0xffffffffu, cta_seen, (int)rank) + warp_scan(run_count, lane) - run_count;
+        total = __shfl_sync(0xffffffffu, c_incl, 31);
+        seen0 = __shfl_sync(0xffffffffu, cta_seen, (int)rank);
+        before0 = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank);
+        landed(total + c_incl + cta_seen, &sh.never);
+    }
+    sync_row();                                                      // nothing of another CTA is read behind this: the others may leave
+    if (warp == 0) {
+        // this CTA's runs
+        const u64 seen = seen0 + warp_scan(run_count, lane) - run_count;
         const u64 ties_run = seen < ties ? min(run_count, ties - seen) : 0;
         const u64 v = run_mass + ties_run * border_w;
-        const u64 before = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank) + warp_scan(v, lane) - v;
+        const u64 before = before0 + warp_scan(v, lane) - v;
         if (lane < p.n_warps) sh.ties_kept[lane] = ties_run;
         if (lane == 0) sh.found_whole = total;
         if (total == 0) {                                            // no candidate
@@ -831,7 +849,6 @@ sample_kernel(SampleParams p)
             ties_left = ties_left > n ? ties_left - n : 0;
         }
     }
-    sync_row();                                                      // nobody leaves while its sums are being read
 }
 
 // ---- BF16 rows: by values
@@ -845,6 +862,7 @@ sample_kernel(SampleParams p)
 // is found by halving the range of keys.
 constexpr int kValues = 4096;
 constexpr int kNearZero = 0x3b00;        // the bits of 2^-9
+constexpr int kMaxSteps = 24;            // a run is at most kMostBytes / 2 / 16 elements
 
 struct SharedValues {
     float warp_max[kMaxWarps];
@@ -861,10 +879,13 @@ struct SharedValues {
     uint32_t key_min, key_max;       // of this CTA
     u64 half_mass;                   // of this CTA, while a range is halved
     uint32_t half_count;
+    uint32_t never;
     u64 found_mass, found_whole;
     uint32_t found_count, found_equal;
     int found_bin;
     u64 ties_kept[kMaxWarps];
+    u64 step_mass[kMaxWarps][kMaxSteps];     // of 256 elements each of a run
+    uint32_t step_count[kMaxWarps][kMaxSteps];
 };
 
 __global__ void __launch_bounds__(32 * kMaxWarps, 2)
@@ -887,6 +908,7 @@ sample_values_kernel(SampleParams p)
     u64* const run_mass = reinterpret_cast<u64*>(count + kValues);
     uint32_t* const run_count = reinterpret_cast<uint32_t*>(run_mass + share);
     auto sync_row = [&]() {
+        __syncwarp();                                                // (the cluster's barrier takes whole warps)
         if (n_ctas > 1) ptx::cluster_sync_all();
         else __syncthreads();
     };
@@ -1016,7 +1038,8 @@ sample_values_kernel(SampleParams p)
             const int at = threadIdx.x * per + j, b = b0 + at;
             if (at < share) {
                 uint32_t c = 0;
-                for (uint32_t r = 0; r < n_ctas; ++r) c += ld_cluster(&count[b], r);
+#pragma unroll
+                for (uint32_t r = 0; r < kMaxCtas; ++r) c += r < n_ctas ? ld_cluster(&count[b], r) : 0u;
                 if (masses && c) {
                     if (is_shared(b)) {
                         for (uint32_t r = 0; r < n_ctas; ++r) sum_m += special_mass(b, r);
@@ -1058,40 +1081,41 @@ sample_values_kernel(SampleParams p)
     // The first bin at which the running count (or mass) reaches `target`: found by one warp of each CTA, told to all.
     auto cross = [&](bool use_mass, u64 target) {
         if (warp == 0) {
-            u64 base_m = 0;
-            uint32_t base_c = 0, here = 0;
+            // the CTA whose share holds the target
+            const u64 s_m = lane < (int)n_ctas ? ld_cluster(&sh.share_mass, (uint32_t)lane) : 0;
+            const uint32_t s_c = lane < (int)n_ctas ? ld_cluster(&sh.share_count, (uint32_t)lane) : 0;
+            const u64 i_m = warp_scan(s_m, lane);
+            const uint32_t i_c = warp_scan(s_c, lane);
+            const unsigned in = __ballot_sync(0xffffffffu, use_mass ? i_m >= target : (u64)i_c >= target);
+            const int r_lane = in ? __ffs(in) - 1 : 31;
+            u64 base_m = __shfl_sync(0xffffffffu, in ? i_m - s_m : i_m, r_lane);
+            uint32_t base_c = __shfl_sync(0xffffffffu, in ? i_c - s_c : i_c, r_lane), here = 0;
             int found = -1;
-            for (uint32_t r = 0; r < n_ctas && found < 0; ++r) {
-                const u64 sm = ld_cluster(&sh.share_mass, r);
-                const uint32_t sc = ld_cluster(&sh.share_count, r);
-                if (use_mass ? base_m + sm >= target : (u64)base_c + sc >= target) {
-                    // 32 places through the share, then the bins between two of them
-                    const int step = share >> 5;
-                    int lo = 0;
-                    for (int wide = step; found < 0; wide = 1) {
-                        const int at = wide > 1 ? (lane + 1) * wide - 1 : lo + lane;
-                        const u64 rm = at < share ? ld_cluster(&run_mass[at], r) : 0;
-                        const uint32_t rc = at < share ? ld_cluster(&run_count[at], r) : 0;
-                        const unsigned hit = __ballot_sync(0xffffffffu, at < share && (use_mass ? base_m + rm >= target : (u64)base_c + rc >= target));
-                        const int src = hit ? __ffs(hit) - 1 : 31;
-                        if (wide > 1) {
-                            lo = src * wide;
-                        } else if (hit || lo + 32 >= share) {
-                            found = lo + src;
-                        } else {
-                            lo += 32;
-                        }
+            if (in) {
+                const uint32_t r = (uint32_t)r_lane;
+                // 32 places through the share, then the bins between two of them
+                const int step = share >> 5;
+                int lo = 0;
+                for (int wide = step; found < 0; wide = 1) {
+                    const int at = wide > 1 ? (lane + 1) * wide - 1 : lo + lane;
+                    const u64 rm = at < share ? ld_cluster(&run_mass[at], r) : 0;
+                    const uint32_t rc = at < share ? ld_cluster(&run_count[at], r) : 0;
+                    const unsigned hit = __ballot_sync(0xffffffffu, at < share && (use_mass ? base_m + rm >= target : (u64)base_c + rc >= target));
+                    const int src = hit ? __ffs(hit) - 1 : 31;
+                    if (wide > 1) {
+                        lo = src * wide;
+                    } else if (hit || lo + 32 >= share) {
+                        found = min(lo + src, share - 1);
+                    } else {
+                        lo += 32;
                     }
-                    const u64 bm = found ? ld_cluster(&run_mass[found - 1], r) : 0;
-                    const uint32_t bc = found ? ld_cluster(&run_count[found - 1], r) : 0;
-                    here = ld_cluster(&run_count[found], r) - bc;
-                    base_m += bm;
-                    base_c += bc;
-                    found += (int)r * share;
-                } else {
-                    base_m += sm;
-                    base_c += sc;
                 }
+                const u64 bm = found ? ld_cluster(&run_mass[found - 1], r) : 0;
+                const uint32_t bc = found ? ld_cluster(&run_count[found - 1], r) : 0;
+                here = ld_cluster(&run_count[found], r) - bc;
+                base_m += bm;
+                base_c += bc;
+                found += (int)r * share;
             }
             if (lane == 0) {
                 sh.found_bin = found;
@@ -1175,6 +1199,7 @@ sample_values_kernel(SampleParams p)
                 mass_k += ld_cluster(&sh.half_mass, r);
                 count_k += ld_cluster(&sh.half_count, r);
             }
+            landed(mass_k + count_k, &sh.never);
             sync_row();
         };
         for (int step = 0; step < 32 && lo < hi; ++step) {
@@ -1225,6 +1250,7 @@ sample_values_kernel(SampleParams p)
                 }
                 sync_row();
                 for (uint32_t r = 0; r < n_ctas; ++r) whole += ld_cluster(&sh.half_mass, r);
+                landed(whole, &sh.never);
                 sync_row();
                 whole += ties * weight(from);
             } else {
@@ -1311,6 +1337,8 @@ sample_values_kernel(SampleParams p)
     const u64 c_incl = warp_scan(c_v, lane);
     const u64 total = __shfl_sync(0xffffffffu, c_incl, 31);
     const u64 seen0 = __shfl_sync(0xffffffffu, c_seen, (int)rank), before0 = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank), mine = __shfl_sync(0xffffffffu, c_v, (int)rank);
+    landed(total + c_incl + c_seen, &sh.never);
+    sync_row();                                                      // nothing of another CTA is read behind this: the others may leave
     const double whole_kept = (double)total;
     auto share_of = [&](float l) {                                   // weight / kept mass
         const double w = l == m ? 1.0 : m_inf ? 0.0 : exp2(((double)l - m_wide) * slope);
@@ -1330,33 +1358,43 @@ sample_values_kernel(SampleParams p)
         holds = target >= before0 && target < before0 + mine;        // this CTA's part holds the token
     }
     if (holds || p.a.probs) {
-        // this CTA's runs: masses above the border, and equals
+        // this CTA's runs, step by step: masses above the border, and equals
+        auto elements = [&](int at, float (&l)[VEC]) {
+            const uint4 q = *reinterpret_cast<const uint4*>(held + (at >> 1));
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) l[j] = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+        };
+        const int steps = p.run / (32 * VEC);
         u64 run_m = 0;
         uint32_t run_c = 0;
-        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
-            const uint4 q = *reinterpret_cast<const uint4*>(held + ((warp0 + i) >> 1));
-            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+        for (int step = 0; step < steps; ++step) {
+            float l[VEC];
+            elements(warp0 + (step * 32 + lane) * VEC, l);
             bool any = false;
+            u64 sum = 0;
+            uint32_t eq = 0;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float l = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
-                any = any || (l >= from && l > border_value);
-                run_c += equals_count && l == border_value ? 1u : 0u;
+                any = any || (l[j] >= from && l[j] > border_value);
+                eq += equals_count && l[j] == border_value ? 1u : 0u;
             }
             if (any) {
                 u64 w[VEC];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) w[j] = kept_above(__uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16));
+                for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float l = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
-                    run_m += l >= from && l > border_value ? w[j] : 0;
-                }
+                for (int j = 0; j < VEC; ++j) sum += l[j] >= from && l[j] > border_value ? w[j] : 0;
+            }
+            sum = warp_sum(sum);
+            eq = __reduce_add_sync(0xffffffffu, eq);
+            run_m += sum;
+            run_c += eq;
+            if (lane == 0) {
+                sh.step_mass[warp][step] = sum;
+                sh.step_count[warp][step] = eq;
             }
         }
-        run_m = warp_sum(run_m);
-        run_c = __reduce_add_sync(0xffffffffu, run_c);
-        __syncthreads();                                             // (warp 0 has read the sums above)
         if (lane == 0) {
             sh.warp_mass[warp] = run_m;
             sh.warp_count[warp] = run_c;
@@ -1371,56 +1409,53 @@ sample_values_kernel(SampleParams p)
             const u64 before = before0 + warp_scan(v, lane) - v;
             if (lane < p.n_warps) sh.ties_kept[lane] = ties_run;
             const unsigned owner = __ballot_sync(0xffffffffu, holds && target >= before && target < before + v);
-            if (owner) {
-                const int src = __ffs(owner) - 1, run0 = src * p.run;
+            if (owner) {                                             // the run, the step in it, the element
+                const int src = __ffs(owner) - 1;
                 u64 left = target - __shfl_sync(0xffffffffu, before, src), ties_left = __shfl_sync(0xffffffffu, ties_run, src);
-                for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
-                    const uint4 q = *reinterpret_cast<const uint4*>(held + ((run0 + i) >> 1));
-                    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
-                    float l[VEC];
-                    uint32_t eq = 0;
+                const u64 s_m = lane < steps ? sh.step_mass[src][lane] : 0, s_c = lane < steps ? sh.step_count[src][lane] : 0;
+                const u64 s_seen = warp_scan(s_c, lane) - s_c;
+                const u64 s_ties = s_seen < ties_left ? min(s_c, ties_left - s_seen) : 0;
+                const u64 s_v = s_m + s_ties * border_w, s_incl = warp_scan(s_v, lane);
+                const unsigned in = __ballot_sync(0xffffffffu, left < s_incl);
+                const int step = in ? __ffs(in) - 1 : 0;
+                left -= __shfl_sync(0xffffffffu, s_incl - s_v, step);
+                ties_left = __shfl_sync(0xffffffffu, s_ties, step);
+                const int at0 = src * p.run + (step * 32 + lane) * VEC;
+                float l[VEC];
+                elements(at0, l);
+                uint32_t eq = 0;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) eq += equals_count && l[j] == border_value ? 1u : 0u;
+                const uint32_t eq_incl = warp_scan(eq, lane);
+                u64 t = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;           // this lane's equals that still count
+                u64 w[VEC], sum = 0;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    if (!(l[j] > border_value)) {
+                        const bool e = equals_count && l[j] == border_value && t > 0;
+                        w[j] = e ? border_w : 0;
+                        t -= e ? 1 : 0;
+                    }
+                    sum += w[j];
+                }
+                const u64 incl = warp_scan(sum, lane);
+                const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
+                if (hit && lane == __ffs(hit) - 1) {
+                    u64 rest = left - (incl - sum);
+                    int at = -1;
+                    float drawn = 0.0f;
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-                        l[j] = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
-                        eq += equals_count && l[j] == border_value ? 1u : 0u;
-                    }
-                    const uint32_t eq_incl = warp_scan(eq, lane);
-                    u64 t = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;       // this lane's equals that still count
-                    u64 w[VEC], sum = 0;
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        if (!(l[j] > border_value)) {
-                            const bool e = equals_count && l[j] == border_value && t > 0;
-                            w[j] = e ? border_w : 0;
-                            t -= e ? 1 : 0;
+                        if (at < 0 && rest < w[j]) {
+                            at = j;
+                            drawn = l[j];
                         }
-                        sum += w[j];
+                        rest -= w[j];
                     }
-                    const u64 incl = warp_scan(sum, lane);
-                    const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
-                    if (hit) {
-                        if (lane == __ffs(hit) - 1) {
-                            u64 rest = left - (incl - sum);
-                            int at = -1;
-                            float drawn = 0.0f;
-#pragma unroll
-                            for (int j = 0; j < VEC; ++j) {
-                                if (at < 0 && rest < w[j]) {
-                                    at = j;
-                                    drawn = l[j];
-                                }
-                                rest -= w[j];
-                            }
-                            p.a.token[row] = cta0 + run0 + i + at - shift;
-                            if (p.a.prob) p.a.prob[row] = share_of(drawn);
-                        }
-                        break;
-                    }
-                    left -= __shfl_sync(0xffffffffu, incl, 31);
-                    const uint32_t eq_all = __shfl_sync(0xffffffffu, eq_incl, 31);
-                    ties_left = ties_left > eq_all ? ties_left - eq_all : 0;
+                    p.a.token[row] = cta0 + at0 + at - shift;
+                    if (p.a.prob) p.a.prob[row] = share_of(drawn);
                 }
             }
         }
@@ -1441,7 +1476,6 @@ sample_values_kernel(SampleParams p)
             ties_left = ties_left > n ? ties_left - n : 0;
         }
     }
-    sync_row();                                                      // nobody leaves while its sums are being read
 }
 
 template <int TYPE>
