@@ -72,8 +72,8 @@ __device__ __forceinline__ u64 ld_cluster(const u64* mine, uint32_t rank)
 }
 
 // A value that was read from another CTA's shared memory has to be here before this thread arrives at the barrier behind which that
-// memory is written again or its CTA is gone; a use of it behind the barrier alone does not see to that (a first build read from
-// CTAs that had left).  So it decides a branch with a store that is never taken: the largest integer is no mass and no key.
+// memory is written again or its CTA is gone, and a use of it behind the barrier alone does not see to that.  So it decides a
+// branch with a store that is never taken: the largest integer is no mass and no key.
 __device__ __forceinline__ void landed(u64 v, uint32_t* never)
 {
     if (v == ~0ull) *reinterpret_cast<volatile uint32_t*>(never) = 1;
@@ -119,7 +119,24 @@ __device__ __forceinline__ u64 exp2_units(double d, double slope, int scale)
     return (u64)__double_as_longlong(__dadd_rn(q, 4503599627370496.0)) & 0xfffffffffffffull;
 }
 
+// What a row was given.  One CTA of the cluster reads it and the others take it from there: their ways through the kernel hang on
+// it, and must be one way even where a caller's program writes these arrays at the wrong time.
+struct RowGiven {
+    float temperature, top_p, min_p, u;
+    int top_k;
+    __device__ void load(const SampleArgs& a, int row)
+    {
+        temperature = a.temperature ? a.temperature[row] : 1.0f;
+        top_p = a.top_p ? a.top_p[row] : 1.0f;
+        min_p = a.min_p ? a.min_p[row] : 0.0f;
+        u = a.u[row];
+        top_k = a.top_k ? a.top_k[row] : 0;
+    }
+};
+__device__ __forceinline__ float ld_cluster_float(const float* v) { return __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(v), 0)); }
+
 struct Shared {
+    RowGiven row;
     uint32_t count[kBins];
     uint32_t plane[3][kBins];        // masses by 15 bits: W & 0x7fff, (W >> 15) & 0x7fff, W >> 30
     // merged over the cluster: running sums through the bins of this CTA's share
@@ -217,12 +234,7 @@ sample_kernel(SampleParams p)
             for (int j = 0; j < VEC; ++j) top = fmaxf(top, widen(q.e[j]));       // fmaxf passes a NaN over
         }
     }
-    const float temperature = p.a.temperature ? p.a.temperature[row] : 1.0f;
-    const int top_k = p.a.top_k ? p.a.top_k[row] : 0;
-    const float top_p = p.a.top_p ? p.a.top_p[row] : 1.0f;
-    const float min_p = p.a.min_p ? p.a.min_p[row] : 0.0f;
-    const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
-    const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
+    if (threadIdx.x == 0 && rank == 0) sh.row.load(p.a, row);
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (lane == 0) sh.warp_max[warp] = top;
@@ -237,6 +249,11 @@ sample_kernel(SampleParams p)
     float m = -INFINITY;
     for (uint32_t r = 0; r < n_ctas; ++r) m = fmaxf(m, __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(&sh.max), r)));
     m += 0.0f;                                                       // (one zero)
+    const float temperature = ld_cluster_float(&sh.row.temperature), top_p = ld_cluster_float(&sh.row.top_p), min_p = ld_cluster_float(&sh.row.min_p);
+    const int top_k = (int)ld_cluster(reinterpret_cast<const uint32_t*>(&sh.row.top_k), 0);
+    const float u_row = ld_cluster_float(&sh.row.u);
+    const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
+    const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
     const bool some = m > -INFINITY;
 
     // ---- weights.  Below `floor_l` they round to zero; with an infinite largest logit, or none but the first largest kept, all
@@ -776,8 +793,7 @@ sample_kernel(SampleParams p)
                 if (p.a.prob) p.a.prob[row] = 0.0f;
             }
         } else {
-            const float u_row = p.a.u[row];
-            const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;     // (a NaN counts as 0)
+                const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;     // (a NaN counts as 0)
             const u64 target = min((u64)((double)u * (double)total), total - 1);
             const unsigned owner = __ballot_sync(0xffffffffu, target >= before && target < before + v);
             if (owner) {                                             // one run of the cluster
@@ -865,6 +881,7 @@ constexpr int kNearZero = 0x3b00;        // the bits of 2^-9
 constexpr int kMaxSteps = 24;            // a run is at most kMostBytes / 2 / 16 elements
 
 struct SharedValues {
+    RowGiven row;
     float warp_max[kMaxWarps];
     float max;                       // of this CTA
     uint32_t special[2][3];          // planes of the masses of the two shared bins, of this CTA
@@ -948,12 +965,7 @@ sample_values_kernel(SampleParams p)
             for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xffff0000u)));
         }
     }
-    const float temperature = p.a.temperature ? p.a.temperature[row] : 1.0f;
-    const int top_k = p.a.top_k ? p.a.top_k[row] : 0;
-    const float top_p = p.a.top_p ? p.a.top_p[row] : 1.0f;
-    const float min_p = p.a.min_p ? p.a.min_p[row] : 0.0f;
-    const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
-    const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
+    if (threadIdx.x == 0 && rank == 0) sh.row.load(p.a, row);
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (lane == 0) sh.warp_max[warp] = top;
@@ -968,6 +980,11 @@ sample_values_kernel(SampleParams p)
     float m = -INFINITY;
     for (uint32_t r = 0; r < n_ctas; ++r) m = fmaxf(m, __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(&sh.max), r)));
     m += 0.0f;                                                       // (one zero)
+    const float temperature = ld_cluster_float(&sh.row.temperature), top_p = ld_cluster_float(&sh.row.top_p), min_p = ld_cluster_float(&sh.row.min_p);
+    const int top_k = (int)ld_cluster(reinterpret_cast<const uint32_t*>(&sh.row.top_k), 0);
+    const float u_row = ld_cluster_float(&sh.row.u);
+    const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
+    const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
     const bool some = m > -INFINITY;
 
     // ---- weights, as above
@@ -1352,7 +1369,6 @@ sample_values_kernel(SampleParams p)
             if (p.a.prob) p.a.prob[row] = 0.0f;
         }
     } else {
-        const float u_row = p.a.u[row];
         const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;         // (a NaN counts as 0)
         target = min((u64)((double)u * whole_kept), total - 1);
         holds = target >= before0 && target < before0 + mine;        // this CTA's part holds the token
