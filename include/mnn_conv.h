@@ -393,9 +393,10 @@ MNN_API void mnn_net_destroy(mnn_net_t net);
  *
  * x [M][ldx], w [N][ldw], bias [N] (NULL = zeros), residual [M][ldr] and y [M][ldy] are of ONE type (opts.type); within a row the
  * elements are contiguous, rows may be any number of elements apart that is not smaller than their length.  Sums, bias,
- * activation and residual are evaluated in fp32 and rounded once, at the store.  fp32 operands enter as TF32 halves (hi*hi +
- * lo*hi + hi*lo, about 22 bits of mantissa); 16-bit operands as they are.  An infinity or NaN in x or w gives what the
- * definition gives.  Pointers need the alignment of their element only; x and w on 16-byte boundaries with row strides of a multiple
+ * activation and residual are evaluated in fp32 and rounded once, at the store.  16-bit operands enter the tensor core as they are,
+ * fp32 operands as two halves (hi*hi + lo*hi + hi*lo): TF32 halves, about 21 bits of each value, or, on PAIRS, FP16 halves of rows
+ * scaled by a power of two, 24 bits of values down to 2^-16 of their row's largest and 2^-39 of the largest below that.  Relative L2
+ * error of fp32 results on normal data: below 1e-6.  An infinity or NaN in x or w gives what the definition gives.  Pointers need the alignment of their element only; x and w on 16-byte boundaries with row strides of a multiple
  * of 16 bytes are read directly, others shifted on the way.  y may be the residual itself (same pointer and stride) and must not
  * overlap x, w or bias.  Nothing is prepared ahead or kept from one run for the next.
  * Rules on pointers, streams and errors as for the convolutions; the current device must be the device of `stream`.
@@ -459,7 +460,7 @@ MNN_API void mnn_linear_destroy(mnn_linear_plan_t plan);
  *                 their whole mass.  u in [0, 1); what lies outside counts as the nearest number inside, a NaN as 0.
  *   prob          w of the token / mass of what stayed.
  *   probs         the same for every i (0 for those that did not stay).
- * Weights are evaluated in fp64 and summed as integers, so that a token does not depend on the order of additions.
+ * Weights are evaluated in fp64 (to 5e-11 of each) and summed as integers, so that a token does not depend on the order of additions.
  *
  * logits [rows][ld] of opts.type, temperature, top_p, min_p, u (float) and top_k (int) are DEVICE arrays of one value per row;
  * each but u may be NULL (temperature 1, nothing cut).  token [rows] int, prob [rows] float or NULL, probs [rows][ld_probs]

@@ -2,10 +2,12 @@
 the MobileNet-v1 conv stack (27 layers) run (a) layer by layer from Python, each layer with its own plan and
 workspace, (b) as ONE mnn_net_run over a shared workspace, (c) as a CUDA-graph replay of that call.
 
-    python -m paper_2002_12418_b200.net_bench [--batch 1] [--reps 50]
+    python -m paper_2002_12418_b200.net_bench [--batch 1] [--reps 50] [--classes 0]
 
 Prints one JSON line with the three times per forward pass (CUDA events, median), the launches per pass and
-the workspace sizes with and without sharing."""
+the workspace sizes with and without sharing.  With --classes C (1000 in the network's own configuration) the pass goes on
+to an answer per image: the features' means through a product with C rows of weights (mnn_linear_run) and one class
+drawn among the five best (mnn_sample_run), timed behind the network and on its own."""
 from __future__ import annotations
 
 import argparse
@@ -23,6 +25,7 @@ def main():
     ap.add_argument("--calibration", default="measure", choices=["measure", "builtin"],
                     help="builtin plans from the library's frozen record (use it under a profiler, which slows "
                          "the calibration's own launches)")
+    ap.add_argument("--classes", type=int, default=0)
     args = ap.parse_args()
     import torch
     B.lib()
@@ -89,6 +92,34 @@ def main():
     ms_graph = timed(graph.replay)
     same_graph = bool(torch.equal(y, y_layers))
     status = net.device_status()
+    answer = {}
+    if args.classes > 0:
+        gen = torch.Generator(device=dev)
+        gen.manual_seed(3999)
+        feats = layers[-1].Cout
+        table = torch.randn(args.classes, feats, generator=gen, device=dev) * feats ** -0.5
+        bias = torch.randn(args.classes, generator=gen, device=dev) * 0.1
+        u = torch.rand(N, generator=gen, device=dev)
+        five = torch.full((N,), 5, dtype=torch.int32, device=dev)
+        head, draw = B.LinearRunner(N, args.classes, feats, "fp32"), B.SampleRunner(N, args.classes, "fp32")
+        logits, token, prob = torch.empty(N, args.classes, device=dev), torch.empty(N, dtype=torch.int32, device=dev), torch.empty(N, device=dev)
+        pooled = torch.empty(N, feats, device=dev)
+
+        def answer_step():
+            torch.mean(y, dim=(2, 3), out=pooled)
+            head.run(pooled, table, bias, y=logits)
+            draw.run(logits, u, top_k=five, token=token, prob=prob)
+
+        ms_answer = timed(answer_step)
+        with_answer = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(with_answer, stream=side):
+                net.run(x, y)
+                answer_step()
+        torch.cuda.synchronize()
+        best = logits.topk(5).indices
+        answer = {"classes": args.classes, "ms_answer": round(ms_answer, 4), "ms_graph_with_answer": round(timed(with_answer.replay), 4),
+                  "drawn_among_the_five_best": bool((best == token[:, None]).any(1).all())}
     flops = sum(l.direct_flops for l in layers)
     print(json.dumps({"workload": "MobileNet-v1 conv stack", "batch": N, "layers": len(layers),
                       "launches_per_pass": net.info.launches_per_run,
@@ -98,7 +129,7 @@ def main():
                       "same_result_net": same, "same_result_graph": same_graph, "device_status": status,
                       "workspace_MB_shared": round(net.info.workspace_bytes / 2 ** 20, 1),
                       "workspace_MB_per_layer_sum": round(net.info.sum_of_layer_workspaces / 2 ** 20, 1),
-                      "activation_buffer_MB": round(net.info.activation_bytes / 2 ** 20, 1)}))
+                      "activation_buffer_MB": round(net.info.activation_bytes / 2 ** 20, 1), **answer}))
 
 
 if __name__ == "__main__":

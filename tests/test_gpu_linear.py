@@ -226,6 +226,27 @@ def test_graph_replay_other_stream_and_two_plans_at_once():
     assert torch.equal(a, want) and torch.equal(b, want)
 
 
+# forms that lay operands out in the workspace first, captured and replayed on new inputs
+@pytest.mark.parametrize("dtype,M,K,N", [("fp32", 1500, 640, 1300), ("bf16", 77, 1001, 513)])
+def test_graph_replay_with_operands_laid_out(dtype, M, K, N):
+    import torch
+    x, w = make(torch, 1, (M, K), K, dtype), make(torch, 2, (N, K), K, dtype)
+    r, other = B.LinearRunner(M, N, K, dtype), B.LinearRunner(M, N, K, dtype)
+    assert r.info.launches_per_run == 2
+    r.run(x, w)
+    torch.cuda.synchronize()
+    y = torch.empty(M, N, dtype=x.dtype, device="cuda")
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        r.run(x, w, y=y)
+        r.run(x, w, y=y)
+    x.mul_(0.5)
+    w.add_(0.25)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, other.run(x, w)) and r.device_status() == 0
+
+
 def test_refusals_of_tensors():
     import torch
     r = B.LinearRunner(4, 8, 16, "bf16", residual="after")

@@ -76,6 +76,20 @@ def test_many_rows():
     check(l, u, top_p=torch.rand(700, generator=g, device="cuda"))
 
 
+# more clusters than run at one time
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_many_rows_of_several_ctas(dtype):
+    import torch
+    rows, vocab = 420, 34001
+    l, u, g = make(torch, 13, rows, vocab, dtype, 1)
+    r = B.SampleRunner(rows, vocab, dtype, ld=vocab + 1)
+    assert r.info.ctas_per_row > 1
+    p = torch.rand(rows, generator=g, device="cuda")
+    k = torch.randint(0, 300, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    check(l, u, probs=False, runner=r, top_p=p)
+    check(l, u, probs=False, runner=r, top_k=k, top_p=p, min_p=p * 0.01)
+
+
 # masks: rows half hidden, rows with one candidate, rows with none; the lowest value of the type instead of -infinity
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("vocab", [50, 9000])
