@@ -40,6 +40,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 1024;
 constexpr int kMaxWarps = 16;
 constexpr int kMaxCtas = 8;
+constexpr int kWindowRun = 256;          // elements of a warp from which on top-p counts first (64 rows of 32000 fp32 40.8 -> 32.9 us)
 constexpr int kGather = 128;             // candidates that are ranked against each other instead of binned again
 constexpr int kMaxScale = 45;
 constexpr int kMostBytes = 176 * 1024;   // of a row's logits in one CTA: the largest vocabulary in fp32 over eight CTAs, and a step of rounding up
@@ -100,7 +101,7 @@ __device__ __forceinline__ V warp_scan(V v, int lane)       // inclusive
 // of degree 6 (minimax by the exchange algorithm, relative error 4.7e-11); additions of 1.5 * 2^52 round to integers.  Every
 // operation is a named one: the sums of several passes are compared with each other, and a multiplication and an addition that
 // the compiler joins in one place and not in another would make two weights of one value.
-__device__ __forceinline__ u64 exp2_units(double d, double slope, int scale)
+__device__ __forceinline__ double exp2_scaled(double d, double slope, int scale)      // 2^(d slope + scale)
 {
     constexpr double kRound = 6755399441055744.0;
     const double y = __dmul_rn(d, slope);
@@ -114,9 +115,12 @@ __device__ __forceinline__ u64 exp2_units(double d, double slope, int scale)
     q = __fma_rn(q, r, 0.24022651066559253);
     q = __fma_rn(q, r, 0.6931471807045294);
     q = __fma_rn(q, r, 1.0);
-    // times 2^(n + scale): an addition to the exponent; the result is below 2^46
-    q = __hiloint2double(__double2hiint(q) + ((__double2loint(t) + scale) << 20), __double2loint(q));
-    return (u64)__double_as_longlong(__dadd_rn(q, 4503599627370496.0)) & 0xfffffffffffffull;
+    // times 2^(n + scale): an addition to the exponent
+    return __hiloint2double(__double2hiint(q) + ((__double2loint(t) + scale) << 20), __double2loint(q));
+}
+__device__ __forceinline__ u64 exp2_units(double d, double slope, int scale)                  // rounded; below 2^46
+{
+    return (u64)__double_as_longlong(__dadd_rn(exp2_scaled(d, slope, scale), 4503599627370496.0)) & 0xfffffffffffffull;
 }
 
 // What a row was given.  One CTA of the cluster reads it and the others take it from there: their ways through the kernel hang on
@@ -219,8 +223,21 @@ sample_kernel(SampleParams p)
     {
         const T* const base = row_ptr - shift;
         const int first = shift, last = shift + p.vocab;             // positions [first, last) are the row
-#pragma unroll 4
-        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+        auto keep = [&](int i, const Piece& q) {
+            *reinterpret_cast<uint4*>(held + warp0 + i) = q.v;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) top = fmaxf(top, widen(q.e[j]));       // fmaxf passes a NaN over
+        };
+        int i = lane * VEC;
+        if (cta0 + warp0 >= first && cta0 + warp0 + p.run <= last)   // a run within the row: no checks, four loads in flight
+            for (; i + 96 * VEC < p.run; i += 128 * VEC) {
+                Piece q[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[j].v = __ldg(reinterpret_cast<const uint4*>(base + cta0 + warp0 + i + j * 32 * VEC));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) keep(i + j * 32 * VEC, q[j]);
+            }
+        for (; i < p.run; i += 32 * VEC) {
             const int at = cta0 + warp0 + i;
             Piece q;
             if (at >= first && at + VEC <= last) {
@@ -229,9 +246,7 @@ sample_kernel(SampleParams p)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) q.e[j] = at + j >= first && at + j < last ? base[at + j] : (T)(-INFINITY);
             }
-            *reinterpret_cast<uint4*>(held + warp0 + i) = q.v;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) top = fmaxf(top, widen(q.e[j]));       // fmaxf passes a NaN over
+            keep(i, q);
         }
     }
     if (threadIdx.x == 0 && rank == 0) sh.row.load(p.a, row);
@@ -314,7 +329,7 @@ sample_kernel(SampleParams p)
         for (int j = 0; j < per; ++j) {
             const int b = b0 + threadIdx.x * per + j;
             if (b < b0 + share) {
-#pragma unroll 2
+#pragma unroll 4
                 for (uint32_t r = 0; r < n_ctas; ++r) {
                     sum_c += ld_cluster(&sh.count[b], r);
                     if (masses)
@@ -438,7 +453,7 @@ sample_kernel(SampleParams p)
     };
     uint32_t border_key = 0, border_equal = 0;                       // the border, and how many elements are equal to it
     // Of the n collected ones, the key at which the running count (or mass) reaches `target`.
-    auto ranked = [&](int n, bool use_mass, u64 target) {
+    auto ranked = [&](int n, bool use_mass, bool masses, u64 target) {
         // 2^g threads of a warp per key
         int g = 0;
         while (g < 5 && n << (g + 1) <= n_threads) ++g;
@@ -450,12 +465,12 @@ sample_kernel(SampleParams p)
             uint32_t more_c = 0, equal = 0;
             for (int j = part; j < n; j += 1 << g) {
                 const uint32_t other = sh.all[j];
-                if (use_mass) more += other > k ? sh.all_mass[j] : 0;
+                if (masses) more += other > k ? sh.all_mass[j] : 0;
                 more_c += other > k ? 1u : 0u;
                 equal += other == k ? 1u : 0u;
             }
             for (int o = 1 << g >> 1; o; o >>= 1) {
-                if (use_mass) more += __shfl_xor_sync(0xffffffffu, more, o);
+                if (masses) more += __shfl_xor_sync(0xffffffffu, more, o);
                 more_c += __shfl_xor_sync(0xffffffffu, more_c, o);
                 equal += __shfl_xor_sync(0xffffffffu, equal, o);
             }
@@ -480,7 +495,7 @@ sample_kernel(SampleParams p)
         if (bin_count <= (uint32_t)kGather) {
             const int n = (int)bin_count;
             collect(n, use_mass, in);
-            ranked(n, use_mass, target);
+            ranked(n, use_mass, use_mass, target);
             return;
         }
         // many: the range of their keys, and a histogram over it, until one key is left
@@ -545,7 +560,9 @@ sample_kernel(SampleParams p)
     if (cut) border_key = key(m);
     u64 run_above = 0;                                               // mass of what lies above `window_top` in this warp's run
     float window_top = INFINITY;
-    if (some && (by_count || by_mass)) {
+    const bool by_window = by_mass && p.run >= kWindowRun;
+    int n_listed = 0;                                                // elements that top-k's search left collected
+    if (some && (by_count || by_window)) {
         for_each([&](float l) {
             if (l > -INFINITY) atomicAdd(&sh.count[bin_of(l)], 1u);
         });
@@ -554,7 +571,14 @@ sample_kernel(SampleParams p)
             cross(false, (u64)top_k);
             if (bin >= 0) {                                          // else fewer candidates than k: all are kept
                 const int b = bin;
-                narrow(false, (u64)top_k, [&](float l) { return l > -INFINITY && bin_of(l) == b; });
+                if (above_count + bin_count <= (uint32_t)kGather) {  // all down to the crossing bin are few: top-p can use them too
+                    n_listed = (int)(above_count + bin_count);
+                    collect(n_listed, by_mass, [&](float l) { return l > -INFINITY && bin_of(l) <= b; });
+                    above_count = 0;
+                    ranked(n_listed, false, by_mass, (u64)top_k);
+                } else {
+                    narrow(false, (u64)top_k, [&](float l) { return l > -INFINITY && bin_of(l) == b; });
+                }
                 ties = (u64)top_k - above_count;
                 cut = true;
             }
@@ -565,17 +589,13 @@ sample_kernel(SampleParams p)
         auto border_target = [&](u64 whole) { return max(1ull, min((u64)ceil((double)fmaxf(top_p, 0.0f) * (double)whole), whole)); };
         u64 target = 0;
         bool done = false;
-        if (cut && above_count + border_equal <= (uint32_t)kGather) {            // few are left by top-k
-            const int n = (int)(above_count + border_equal);
-            const float from = value_of_key(border_key);
-            u64 whole = collect(n, true, [&](float l) { return l >= from; });
-            whole -= ((u64)n - (u64)top_k) * weight(from);
-            target = border_target(whole);
+        if (n_listed) {                                              // few are left by top-k
+            target = border_target(above_mass + ties * weight(value_of_key(border_key)));
             above_mass = 0;
             above_count = 0;
-            ranked(n, true, target);
+            ranked(n_listed, true, true, target);
             done = true;
-        } else if (!cut) {
+        } else if (by_window && !cut) {
             // where the border must lie, by the counts and the weights in the middle of the bins
             const float s = (float)slope;
             auto middle = [&](int b) { return b == 0 ? 1.0f : exp2f(-s * __uint_as_float((uint32_t)((b + kFirstBin) << 17) + (1u << 16))); };
@@ -601,7 +621,7 @@ sample_kernel(SampleParams p)
                 for (int j = 0; j < per; ++j) {
                     run += estimate(threadIdx.x * per + j);
                     if (run > guess || j + 1 == per) {
-                        sh.found_bin = threadIdx.x * per + j;
+                        atomicMin(&sh.found_bin, (int)threadIdx.x * per + j);        // (two neighbours may claim it by their rounding)
                         break;
                     }
                 }
@@ -761,9 +781,9 @@ sample_kernel(SampleParams p)
         }
     }
     sync_row();
-    auto share_of = [&](float l, double whole) {                     // weight / kept mass
-        const double w = l == m ? 1.0 : m_inf ? 0.0 : exp2(((double)l - m_wide) * slope);
-        return (float)(w * (double)unit / whole);
+    auto share_of = [&](float l, double per_whole) {                 // weight / kept mass
+        const double d = l == m ? 0.0 : (double)l - m_wide;
+        return m_inf && l != m ? 0.0f : (float)(exp2_scaled(fmax(d * slope, -1000.0), 1.0, 0) * per_whole);
     };
     u64 total = 0, before0 = 0, seen0 = 0;
     if (warp == 0) {
@@ -835,7 +855,7 @@ sample_kernel(SampleParams p)
                                 if (rest < here) {
                                     found = true;
                                     p.a.token[row] = cta0 + run0 + i + j - shift;
-                                    if (p.a.prob) p.a.prob[row] = share_of(l, (double)total);
+                                    if (p.a.prob) p.a.prob[row] = share_of(l, (double)unit / (double)total);
                                 }
                                 rest -= here;
                             }
@@ -853,14 +873,14 @@ sample_kernel(SampleParams p)
         __syncthreads();
         float* const out = p.a.probs + (long long)row * p.ld_probs;
         u64 ties_left = sh.ties_kept[warp];
-        const double whole = (double)sh.found_whole;
+        const double whole = (double)sh.found_whole, per_whole = (double)unit / whole;
         for (int i = lane; i < p.run; i += 32) {
             const int at = cta0 + warp0 + i - shift;
             const float l = widen(held[warp0 + i]);
             const bool eq = equals_count && l == border_value;
             const unsigned eqs = __ballot_sync(0xffffffffu, eq);
             const bool keep = l > border_value ? (least == 0 || weight(l) >= least) : eq && (u64)__popc(eqs & ((1u << lane) - 1u)) < ties_left;
-            if (at >= 0 && at < p.vocab) out[at] = keep && whole > 0.0 ? share_of(l, whole) : 0.0f;
+            if (at >= 0 && at < p.vocab) out[at] = keep && whole > 0.0 ? share_of(l, per_whole) : 0.0f;
             const u64 n = (u64)__popc(eqs);
             ties_left = ties_left > n ? ties_left - n : 0;
         }
@@ -943,8 +963,22 @@ sample_values_kernel(SampleParams p)
     {
         const unsigned short* const base = reinterpret_cast<const unsigned short*>(row_ptr) - shift;
         const int first = shift, last = shift + p.vocab;
-#pragma unroll 4
-        for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
+        auto keep = [&](int i, const uint4& q) {
+            *reinterpret_cast<uint4*>(held + ((warp0 + i) >> 1)) = q;
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xffff0000u)));
+        };
+        int i = lane * VEC;
+        if (cta0 + warp0 >= first && cta0 + warp0 + p.run <= last)
+            for (; i + 96 * VEC < p.run; i += 128 * VEC) {
+                uint4 q[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[j] = __ldg(reinterpret_cast<const uint4*>(base + cta0 + warp0 + i + j * 32 * VEC));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) keep(i + j * 32 * VEC, q[j]);
+            }
+        for (; i < p.run; i += 32 * VEC) {
             const int at = cta0 + warp0 + i;
             uint4 q;
             if (at >= first && at + VEC <= last) {
@@ -959,10 +993,7 @@ sample_values_kernel(SampleParams p)
                 }
                 q = make_uint4(u[0], u[1], u[2], u[3]);
             }
-            *reinterpret_cast<uint4*>(held + ((warp0 + i) >> 1)) = q;
-            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xffff0000u)));
+            keep(i, q);
         }
     }
     if (threadIdx.x == 0 && rank == 0) sh.row.load(p.a, row);
@@ -1356,10 +1387,10 @@ sample_values_kernel(SampleParams p)
     const u64 seen0 = __shfl_sync(0xffffffffu, c_seen, (int)rank), before0 = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank), mine = __shfl_sync(0xffffffffu, c_v, (int)rank);
     landed(total + c_incl + c_seen, &sh.never);
     sync_row();                                                      // nothing of another CTA is read behind this: the others may leave
-    const double whole_kept = (double)total;
+    const double whole_kept = (double)total, per_whole = (double)unit / whole_kept;
     auto share_of = [&](float l) {                                   // weight / kept mass
-        const double w = l == m ? 1.0 : m_inf ? 0.0 : exp2(((double)l - m_wide) * slope);
-        return (float)(w * (double)unit / whole_kept);
+        const double d = l == m ? 0.0 : (double)l - m_wide;
+        return m_inf && l != m ? 0.0f : (float)(exp2_scaled(fmax(d * slope, -1000.0), 1.0, 0) * per_whole);
     };
     u64 target = 0;
     bool holds = false;
@@ -1520,12 +1551,16 @@ SampleTiling sample_tiling(const SampleShape& s, int num_sms)
     SampleTiling t;
     const int size = s.type == MNN_TYPE_FP32 ? 4 : 2, vec = 16 / size;
     const long long span = (long long)s.vocab + vec - 1;             // with the positions before an unaligned row
-    // CTAs per row: as many as leave each 64 KB, so that two are resident per SM, and more while SMs idle and every CTA keeps
+    // CTAs per row: as many as leave each a size at which two are resident per SM, and more while SMs idle and every CTA keeps
     // 4096 elements
     t.ctas = 1;
-    while (t.ctas < kMaxCtas && ((span + t.ctas - 1) / t.ctas * size > 66 * 1024 ||
-                                 ((long long)s.rows * t.ctas <= num_sms && span / (2 * t.ctas) >= 4096)))
+    while (t.ctas < kMaxCtas) {
+        const long long logits = (span + t.ctas - 1) / t.ctas * size;
+        const long long sums = s.type == MNN_TYPE_BF16 ? kValues * 4 + kValues * 12 / t.ctas : 33 * 1024;
+        const bool idle = (long long)s.rows * t.ctas <= num_sms && span / (2 * t.ctas) >= 4096;
+        if (logits + sums <= 100 * 1024 && !idle) break;
         t.ctas *= 2;
+    }
     const long long per_cta = (span + t.ctas - 1) / t.ctas;
     t.warps = per_cta > 2048 ? 16 : 8;
     const int step = 32 * vec;

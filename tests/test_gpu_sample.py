@@ -80,7 +80,7 @@ def test_many_rows():
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_many_rows_of_several_ctas(dtype):
     import torch
-    rows, vocab = 420, 34001
+    rows, vocab = 420, 50001
     l, u, g = make(torch, 13, rows, vocab, dtype, 1)
     r = B.SampleRunner(rows, vocab, dtype, ld=vocab + 1)
     assert r.info.ctas_per_row > 1
