@@ -350,7 +350,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
     } else if (F32) {
         // converters: the low halves of both tiles, in the same (swizzled) places
-        constexpr int kPer = kAux / Roles<TYPE, COPY>::kGroups;          // warps of a group
+        constexpr int kPer = F32 ? kAux / Roles<TYPE, COPY>::kGroups : 1;     // warps of a group
         const int w = warp - 2 - kEpiWarps, group = w / kPer, t = (w - group * kPer) * 32 + lane;
         uint32_t stage = 0, phase = 0;
         int turn = 0;
@@ -468,9 +468,10 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     const int eb = f32 ? 4 : 2;
     const bool strides = (s.ldx * eb) % 16 != 0 || (s.ldw * eb) % 16 != 0, copy = unaligned || strides;
     LinearTiling t = {};
-    if (s.M <= 4) {
+    if (s.M <= 2 || (s.M <= 4 && (long long)s.N * s.K * eb <= 6 << 20)) {
         // up to four rows: a stream of w (linear_few.cu); two features a warp, and one, and several warps per K loop, where that
-        // leaves fewer than 16 warps per SM
+        // leaves fewer than 16 warps per SM.  With three or four rows the sums cost more than the stream once w is large: 4 x 4096 x
+        // 4096 BF16 12.3 us here and 8.4 on tiles, 4 x 1024 x 1000 3.5 and 5.1, two rows 6.9 and 8.2.
         t.form = MNN_LINEAR_FEW;
         t.bm = s.M;
         t.feats = s.M > 2 || s.N / 2 >= 16ll * num_sms ? 2 : 1;
