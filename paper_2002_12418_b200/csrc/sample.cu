@@ -40,6 +40,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 1024;
 constexpr int kMaxWarps = 16;
 constexpr int kMaxCtas = 8;
+constexpr int kMaxSteps = 24;            // steps of 32 pieces of 16 bytes in a run: at most kMostBytes / 16 / 512, and one of rounding up
 constexpr int kWindowRun = 256;          // elements of a warp from which on top-p counts first (64 rows of 32000 fp32 40.8 -> 32.9 us)
 constexpr int kGather = 128;             // candidates that are ranked against each other instead of binned again
 constexpr int kMaxScale = 45;
@@ -78,6 +79,23 @@ __device__ __forceinline__ u64 ld_cluster(const u64* mine, uint32_t rank)
 __device__ __forceinline__ void landed(u64 v, uint32_t* never)
 {
     if (v == ~0ull) *reinterpret_cast<volatile uint32_t*>(never) = 1;
+}
+
+// One value of every CTA, all reads in flight together; 0 for CTAs that are not there.
+template <typename V>
+__device__ __forceinline__ void ld_all(const V* mine, uint32_t n_ctas, V (&v)[kMaxCtas])
+{
+#pragma unroll
+    for (uint32_t r = 0; r < kMaxCtas; ++r) v[r] = r < n_ctas ? ld_cluster(mine, r) : (V)0;
+}
+template <typename V>
+__device__ __forceinline__ V sum_all(const V* mine, uint32_t n_ctas)
+{
+    V v[kMaxCtas], sum = 0;
+    ld_all(mine, n_ctas, v);
+#pragma unroll
+    for (int r = 0; r < kMaxCtas; ++r) sum += v[r];
+    return sum;
 }
 
 __device__ __forceinline__ u64 warp_sum(u64 v)
@@ -121,6 +139,42 @@ __device__ __forceinline__ double exp2_scaled(double d, double slope, int scale)
 __device__ __forceinline__ u64 exp2_units(double d, double slope, int scale)                  // rounded; below 2^46
 {
     return (u64)__double_as_longlong(__dadd_rn(exp2_scaled(d, slope, scale), 4503599627370496.0)) & 0xfffffffffffffull;
+}
+
+// The element of a step of 32 * VEC: in one lane the index of its element at which the running mass exceeds `left`, in the others -1.
+// `ties` equals of the border still count in this step; what lies above the border weighs `kept`.
+template <int VEC, typename Kept>
+__device__ __forceinline__ int draw_element(const float (&l)[VEC], u64 left, u64 ties, float border_value, bool equals_count, u64 border_w, int lane, Kept&& kept)
+{
+    uint32_t eq = 0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) eq += equals_count && l[j] == border_value ? 1u : 0u;
+    const uint32_t eq_incl = warp_scan(eq, lane);
+    u64 t = ties > eq_incl - eq ? ties - (eq_incl - eq) : 0;         // this lane's equals that still count
+    u64 w[VEC], sum = 0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) w[j] = kept(l[j]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        if (!(l[j] > border_value)) {
+            const bool e = equals_count && l[j] == border_value && t > 0;
+            w[j] = e ? border_w : 0;
+            t -= e ? 1 : 0;
+        }
+        sum += w[j];
+    }
+    const u64 incl = warp_scan(sum, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
+    int at = -1;
+    if (hit && lane == __ffs(hit) - 1) {
+        u64 rest = left - (incl - sum);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            if (at < 0 && rest < w[j]) at = j;
+            rest -= w[j];
+        }
+    }
+    return at;
 }
 
 // What a row was given.  One CTA of the cluster reads it and the others take it from there: their ways through the kernel hang on
@@ -169,6 +223,8 @@ struct Shared {
     uint32_t found_count, found_key, found_equal;
     int found_bin;
     u64 ties_kept[kMaxWarps];
+    u64 step_mass[kMaxSteps];        // of 32 pieces each of the run that holds the token
+    uint32_t step_count[kMaxSteps];
 };
 
 struct SampleParams {
@@ -262,7 +318,13 @@ sample_kernel(SampleParams p)
     }
     sync_row();
     float m = -INFINITY;
-    for (uint32_t r = 0; r < n_ctas; ++r) m = fmaxf(m, __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(&sh.max), r)));
+    {
+        uint32_t tops[kMaxCtas];
+        ld_all(reinterpret_cast<const uint32_t*>(&sh.max), n_ctas, tops);
+#pragma unroll
+        for (uint32_t r = 0; r < kMaxCtas; ++r)
+            if (r < n_ctas) m = fmaxf(m, __uint_as_float(tops[r]));
+    }
     m += 0.0f;                                                       // (one zero)
     const float temperature = ld_cluster_float(&sh.row.temperature), top_p = ld_cluster_float(&sh.row.top_p), min_p = ld_cluster_float(&sh.row.min_p);
     const int top_k = (int)ld_cluster(reinterpret_cast<const uint32_t*>(&sh.row.top_k), 0);
@@ -329,11 +391,19 @@ sample_kernel(SampleParams p)
         for (int j = 0; j < per; ++j) {
             const int b = b0 + threadIdx.x * per + j;
             if (b < b0 + share) {
-#pragma unroll 4
-                for (uint32_t r = 0; r < n_ctas; ++r) {
-                    sum_c += ld_cluster(&sh.count[b], r);
-                    if (masses)
-                        sum_m += (u64)ld_cluster(&sh.plane[0][b], r) + ((u64)ld_cluster(&sh.plane[1][b], r) << 15) + ((u64)ld_cluster(&sh.plane[2][b], r) << 30);
+                if (n_ctas == 1) {
+                    sum_c += sh.count[b];
+                    if (masses) sum_m += (u64)sh.plane[0][b] + ((u64)sh.plane[1][b] << 15) + ((u64)sh.plane[2][b] << 30);
+                } else {
+                    sum_c += sum_all(&sh.count[b], n_ctas);
+                }
+                if (masses && n_ctas > 1) {                          // (a plane's sum over the cluster may pass 32 bits)
+                    uint32_t w0[kMaxCtas], w1[kMaxCtas], w2[kMaxCtas];
+                    ld_all(&sh.plane[0][b], n_ctas, w0);
+                    ld_all(&sh.plane[1][b], n_ctas, w1);
+                    ld_all(&sh.plane[2][b], n_ctas, w2);
+#pragma unroll
+                    for (int r = 0; r < kMaxCtas; ++r) sum_m += (u64)w0[r] + ((u64)w1[r] << 15) + ((u64)w2[r] << 30);
                 }
                 sh.run_mass[b] = sum_m;                              // (running within this thread; the rest is added below)
                 sh.run_count[b] = sum_c;
@@ -425,14 +495,17 @@ sample_kernel(SampleParams p)
         });
         sync_row();
         u64 sum = 0;
+        uint32_t have[kMaxCtas];
+        ld_all(&sh.n_list, n_ctas, have);
         for (int at = threadIdx.x; at < n; at += n_threads) {
             int i = at;
             uint32_t r = 0;
-            for (; r + 1 < n_ctas; ++r) {
-                const int have = (int)ld_cluster(&sh.n_list, r);
-                if (i < have) break;
-                i -= have;
-            }
+#pragma unroll
+            for (uint32_t c = 0; c + 1 < kMaxCtas; ++c)
+                if (r == c && c + 1 < n_ctas && i >= (int)have[c]) {
+                    i -= (int)have[c];
+                    r = c + 1;
+                }
             const uint32_t k = ld_cluster(&sh.list[i], r);
             const u64 w = masses ? weight(value_of_key(k)) : 0;
             sh.all[at] = k;
@@ -669,10 +742,8 @@ sample_kernel(SampleParams p)
             u64 whole = 0;
             above_mass = 0;
             above_count = 0;
-            for (uint32_t r = 0; r < n_ctas; ++r) {
-                above_mass += ld_cluster(&sh.cta_above, r);
-                whole += ld_cluster(&sh.cta_mass, r);
-            }
+            above_mass = sum_all(&sh.cta_above, n_ctas);
+            whole = sum_all(&sh.cta_mass, n_ctas);
             target = border_target(whole);
             if (above_mass < target) {
                 cross(true, target);
@@ -702,8 +773,7 @@ sample_kernel(SampleParams p)
                 }
             });
             merge(true);
-            u64 whole = 0;
-            for (uint32_t r = 0; r < n_ctas; ++r) whole += ld_cluster(&sh.share_mass, r);
+            u64 whole = sum_all(&sh.share_mass, n_ctas);
             if (surplus) whole -= surplus * weight(from);
             target = border_target(whole);
             above_mass = 0;
@@ -785,7 +855,8 @@ sample_kernel(SampleParams p)
         const double d = l == m ? 0.0 : (double)l - m_wide;
         return m_inf && l != m ? 0.0f : (float)(exp2_scaled(fmax(d * slope, -1000.0), 1.0, 0) * per_whole);
     };
-    u64 total = 0, before0 = 0, seen0 = 0;
+    u64 total = 0, before0 = 0, seen0 = 0, left = 0, ties_left = 0;
+    int found_run = -1;
     if (warp == 0) {
         // the CTAs' sums, with as many equals as still count
         const u64 c_m = lane < (int)n_ctas ? ld_cluster(&sh.cta_mass, (uint32_t)lane) : 0;
@@ -813,66 +884,69 @@ sample_kernel(SampleParams p)
                 if (p.a.prob) p.a.prob[row] = 0.0f;
             }
         } else {
-                const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;     // (a NaN counts as 0)
+            const float u = u_row > 0.0f ? fminf(u_row, 0.99999994f) : 0.0f;     // (a NaN counts as 0)
             const u64 target = min((u64)((double)u * (double)total), total - 1);
             const unsigned owner = __ballot_sync(0xffffffffu, target >= before && target < before + v);
             if (owner) {                                             // one run of the cluster
-                const int src = __ffs(owner) - 1, run0 = src * p.run;
-                u64 left = target - __shfl_sync(0xffffffffu, before, src), ties_left = __shfl_sync(0xffffffffu, ties_run, src);
-                for (int i = lane * VEC; i < p.run; i += 32 * VEC) {
-                    Piece q;
-                    q.v = *reinterpret_cast<const uint4*>(held + run0 + i);
-                    uint32_t eq = 0;
+                found_run = __ffs(owner) - 1;
+                left = target - __shfl_sync(0xffffffffu, before, found_run);
+                ties_left = __shfl_sync(0xffffffffu, ties_run, found_run);
+            }
+        }
+        if (lane == 0) sh.found_bin = found_run;
+    }
+    __syncthreads();
+    const int drawn_run = sh.found_bin;
+    if (drawn_run >= 0) {                                            // this CTA holds the token: the run's steps by all warps
+        const int run0 = drawn_run * p.run, steps = p.run / (32 * VEC);
+        auto elements = [&](int step, float (&l)[VEC]) {
+            Piece q;
+            q.v = *reinterpret_cast<const uint4*>(held + run0 + (step * 32 + lane) * VEC);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) eq += equals_count && widen(q.e[j]) == border_value ? 1u : 0u;
-                    const uint32_t eq_incl = warp_scan(eq, lane);
-                    // the weight of an element, where this lane's first `lane_ties` equals of the border still count
-                    const u64 lane_ties = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;
-                    auto kept_weight = [&](float l, u64 w, u64& t) -> u64 {
-                        if (l > border_value) return w;
-                        if (equals_count && l == border_value && t > 0) {
-                            --t;
-                            return border_w;
-                        }
-                        return 0;
-                    };
-                    u64 sum = 0, t = lane_ties, w[VEC];
+            for (int j = 0; j < VEC; ++j) l[j] = widen(q.e[j]);
+        };
+        for (int step = warp; step < steps; step += p.n_warps) {
+            float l[VEC];
+            elements(step, l);
+            u64 w[VEC], sum = 0;
+            uint32_t eq = 0;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) w[j] = kept_above(widen(q.e[j]));
+            for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) sum += kept_weight(widen(q.e[j]), w[j], t);
-                    const u64 incl = warp_scan(sum, lane);
-                    const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
-                    if (hit) {
-                        if (lane == __ffs(hit) - 1) {
-                            u64 rest = left - (incl - sum);
-                            bool found = false;
-                            t = lane_ties;
-#pragma unroll 1
-                            for (int j = 0; j < VEC && !found; ++j) {
-                                const float l = widen(held[run0 + i + j]);
-                                const u64 here = kept_weight(l, kept_above(l), t);
-                                if (rest < here) {
-                                    found = true;
-                                    p.a.token[row] = cta0 + run0 + i + j - shift;
-                                    if (p.a.prob) p.a.prob[row] = share_of(l, (double)unit / (double)total);
-                                }
-                                rest -= here;
-                            }
-                        }
-                        break;
-                    }
-                    left -= __shfl_sync(0xffffffffu, incl, 31);
-                    const uint32_t eq_all = __shfl_sync(0xffffffffu, eq_incl, 31);
-                    ties_left = ties_left > eq_all ? ties_left - eq_all : 0;
-                }
+            for (int j = 0; j < VEC; ++j) {
+                sum += l[j] > border_value ? w[j] : 0;
+                eq += equals_count && l[j] == border_value ? 1u : 0u;
+            }
+            sum = warp_sum(sum);
+            eq = __reduce_add_sync(0xffffffffu, eq);
+            if (lane == 0) {
+                sh.step_mass[step] = sum;
+                sh.step_count[step] = eq;
+            }
+        }
+        __syncthreads();
+        if (warp == 0) {
+            const u64 s_m = lane < steps ? sh.step_mass[lane] : 0, s_c = lane < steps ? sh.step_count[lane] : 0;
+            const u64 s_seen = warp_scan(s_c, lane) - s_c;
+            const u64 s_ties = s_seen < ties_left ? min(s_c, ties_left - s_seen) : 0;
+            const u64 s_v = s_m + s_ties * border_w, s_incl = warp_scan(s_v, lane);
+            const unsigned in = __ballot_sync(0xffffffffu, left < s_incl);
+            const int step = in ? __ffs(in) - 1 : 0;
+            float l[VEC];
+            elements(step, l);
+            const int at = draw_element<VEC>(l, left - __shfl_sync(0xffffffffu, s_incl - s_v, step), __shfl_sync(0xffffffffu, s_ties, step), border_value,
+                                             equals_count, border_w, lane, kept_above);
+            if (at >= 0) {
+                const int index = run0 + (step * 32 + lane) * VEC + at;
+                p.a.token[row] = cta0 + index - shift;
+                if (p.a.prob) p.a.prob[row] = share_of(widen(held[index]), (double)unit / (double)total);
             }
         }
     }
     if (p.a.probs) {                                                 // the whole filtered distribution
         __syncthreads();
         float* const out = p.a.probs + (long long)row * p.ld_probs;
-        u64 ties_left = sh.ties_kept[warp];
+        ties_left = sh.ties_kept[warp];
         const double whole = (double)sh.found_whole, per_whole = (double)unit / whole;
         for (int i = lane; i < p.run; i += 32) {
             const int at = cta0 + warp0 + i - shift;
@@ -898,7 +972,6 @@ sample_kernel(SampleParams p)
 // is found by halving the range of keys.
 constexpr int kValues = 4096;
 constexpr int kNearZero = 0x3b00;        // the bits of 2^-9
-constexpr int kMaxSteps = 24;            // a run is at most kMostBytes / 2 / 16 elements
 
 struct SharedValues {
     RowGiven row;
@@ -1009,7 +1082,13 @@ sample_values_kernel(SampleParams p)
     }
     sync_row();
     float m = -INFINITY;
-    for (uint32_t r = 0; r < n_ctas; ++r) m = fmaxf(m, __uint_as_float(ld_cluster(reinterpret_cast<const uint32_t*>(&sh.max), r)));
+    {
+        uint32_t tops[kMaxCtas];
+        ld_all(reinterpret_cast<const uint32_t*>(&sh.max), n_ctas, tops);
+#pragma unroll
+        for (uint32_t r = 0; r < kMaxCtas; ++r)
+            if (r < n_ctas) m = fmaxf(m, __uint_as_float(tops[r]));
+    }
     m += 0.0f;                                                       // (one zero)
     const float temperature = ld_cluster_float(&sh.row.temperature), top_p = ld_cluster_float(&sh.row.top_p), min_p = ld_cluster_float(&sh.row.min_p);
     const int top_k = (int)ld_cluster(reinterpret_cast<const uint32_t*>(&sh.row.top_k), 0);
@@ -1086,8 +1165,7 @@ sample_values_kernel(SampleParams p)
             const int at = threadIdx.x * per + j, b = b0 + at;
             if (at < share) {
                 uint32_t c = 0;
-#pragma unroll
-                for (uint32_t r = 0; r < kMaxCtas; ++r) c += r < n_ctas ? ld_cluster(&count[b], r) : 0u;
+                c = n_ctas == 1 ? count[b] : sum_all(&count[b], n_ctas);
                 if (masses && c) {
                     if (is_shared(b)) {
                         for (uint32_t r = 0; r < n_ctas; ++r) sum_m += special_mass(b, r);
@@ -1302,7 +1380,7 @@ sample_values_kernel(SampleParams p)
                 sync_row();
                 whole += ties * weight(from);
             } else {
-                for (uint32_t r = 0; r < n_ctas; ++r) whole += ld_cluster(&sh.share_mass, r);
+                whole = sum_all(&sh.share_mass, n_ctas);
             }
             // kept while the mass before < p * whole: up to where the running mass reaches ceil(p * whole)
             const u64 target = max(1ull, min((u64)ceil((double)fmaxf(top_p, 0.0f) * (double)whole), whole));
@@ -1470,37 +1548,11 @@ sample_values_kernel(SampleParams p)
                 const int at0 = src * p.run + (step * 32 + lane) * VEC;
                 float l[VEC];
                 elements(at0, l);
-                uint32_t eq = 0;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) eq += equals_count && l[j] == border_value ? 1u : 0u;
-                const uint32_t eq_incl = warp_scan(eq, lane);
-                u64 t = ties_left > eq_incl - eq ? ties_left - (eq_incl - eq) : 0;           // this lane's equals that still count
-                u64 w[VEC], sum = 0;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) w[j] = kept_above(l[j]);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    if (!(l[j] > border_value)) {
-                        const bool e = equals_count && l[j] == border_value && t > 0;
-                        w[j] = e ? border_w : 0;
-                        t -= e ? 1 : 0;
-                    }
-                    sum += w[j];
-                }
-                const u64 incl = warp_scan(sum, lane);
-                const unsigned hit = __ballot_sync(0xffffffffu, incl > left);
-                if (hit && lane == __ffs(hit) - 1) {
-                    u64 rest = left - (incl - sum);
-                    int at = -1;
+                const int at = draw_element<VEC>(l, left, ties_left, border_value, equals_count, border_w, lane, kept_above);
+                if (at >= 0) {
                     float drawn = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        if (at < 0 && rest < w[j]) {
-                            at = j;
-                            drawn = l[j];
-                        }
-                        rest -= w[j];
-                    }
+                    for (int j = 0; j < VEC; ++j) drawn = at == j ? l[j] : drawn;
                     p.a.token[row] = cta0 + at0 + at - shift;
                     if (p.a.prob) p.a.prob[row] = share_of(drawn);
                 }
