@@ -25,8 +25,9 @@ namespace {
 constexpr int kRows = 128;               // rows of w per CTA and stage
 constexpr int kPairN = 256;              // columns of tensor memory per accumulator: at most so many rows of x per work item
 constexpr int kSegment = 2;              // fp32: blocks of 64 elements of K between additions to the registers
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+// epilogue warps, two to a quarter of the lanes; four for fp32, whose sums stay in registers (128 to a thread were too many)
+template <int TYPE> constexpr int kEpiWarps = TYPE == MNN_TYPE_FP32 ? 16 : 8;
+template <int TYPE> constexpr int kThreads = 64 + 32 * kEpiWarps<TYPE>;
 constexpr int kMaxStages = 6;
 constexpr uint32_t kTileBytes = kRows * 128;
 constexpr int kSmem = 200 * 1024;        // one CTA per SM
@@ -77,7 +78,7 @@ __device__ __forceinline__ void pair_commit(uint32_t bar)
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads<TYPE>, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                    const __grid_constant__ CUtensorMap map_x_low, const __grid_constant__ CUtensorMap map_w_low, PairLinearParams p)
 {
@@ -105,7 +106,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         }
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(ptx::smem_u32(&tfull_bar[s]), 1);
-            ptx::mbar_init(ptx::smem_u32(&tempty_bar[s]), 2 * kEpiWarps);
+            ptx::mbar_init(ptx::smem_u32(&tempty_bar[s]), 2 * kEpiWarps<TYPE>);
         }
         abort_flag = 0;
         ptx::fence_barrier_init();
@@ -210,8 +211,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         }
     } else {
         const int q = warp & 3;                       // tensor-memory lane quarter this warp may read
-        const int n_chunks = p.bm >> 4, per_part = (n_chunks + 1) >> 1;
-        const int ch0 = ((warp - 2) >> 2) * per_part, ch1 = min(ch0 + per_part, n_chunks);         // its half of the chunks of 16 rows
+        constexpr int kParts = kEpiWarps<TYPE> / 4;
+        const int n_chunks = p.bm >> 4, per_part = (n_chunks + kParts - 1) / kParts;
+        const int ch0 = ((warp - 2) >> 2) * per_part, ch1 = min(ch0 + per_part, n_chunks);         // its share of the chunks of 16 rows
         uint32_t acc = 0, acc_phase = 0;
         auto wait_acc = [&]() {
             int got = 1;
@@ -240,11 +242,17 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             auto rows_at = [&](int ch) { return (int)min(16ll, p.M - (m_item + ch * 16)); };
             if (F32) {
                 const int w_up = n_ok ? __ldg(p.w_up + n) : 0;
-                float sum[8][16];                     // at most 128 of the 256 columns belong to this warp
+                float sum[4][16];                     // at most 64 of the 256 columns belong to this warp
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) sum[c][j] = 0.0f;
+                // the residual's lines come into L2 while the product runs (its values would take the sums' registers)
+                if (p.epi.res_mode != MNN_RESIDUAL_NONE) {
+                    const float* r = static_cast<const float*>(p.epi.residual) + min(n - lane, p.N - 1);
+                    for (int j = ch0 * 16 + lane; j < ch1 * 16; j += 32)
+                        if (m_item + j < p.M) asm volatile("prefetch.global.L2 [%0];" ::"l"(r + (m_item + j) * p.epi.ldr));
+                }
                 for (int seg = 0; seg < p.k_blocks; seg += kSegment) {
                     if (!wait_acc()) {
                         ok = false;
@@ -252,7 +260,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     }
                     const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * (uint32_t)kPairN;
 #pragma unroll
-                    for (int c = 0; c < 8; c += 2)
+                    for (int c = 0; c < 4; c += 2)
                         if (ch0 + c < ch1) {          // (an odd last chunk's partner is read too, and not used)
                             uint32_t va[16], vb[16];
                             ptx::tmem_ld16(taddr + (uint32_t)((ch0 + c) * 16), va);
@@ -268,21 +276,30 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
+                for (int c = 0; c < 4; ++c)
                     if (ch0 + c < ch1) {
                         const long long m0 = m_item + (ch0 + c) * 16;
                         const int rows = rows_at(ch0 + c);
-                        out.fetch(p.epi, m0, rows, n, n_ok);
-                        if (n_ok) {                   // the scales of x's and w's rows undone: in two steps, each within fp32's exponents
+                        // the scales of x's and w's rows undone: in two steps, each within fp32's exponents.  (A lane reads one
+                        // row's exponent and the others take it from there.)
+                        const int ups = __ldg(p.x_up + min(m0 + (lane & 15), (long long)p.M - 1));
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if (j < rows) {
-                                    const int down = -(w_up + __ldg(p.x_up + m0 + j)), half = down >> 1;
-                                    sum[c][j] = sum[c][j] * power_of_two(half) * power_of_two(down - half);
-                                }
+                        for (int j = 0; j < 16; ++j) {
+                            const int down = -(w_up + __shfl_sync(0xffffffffu, ups, j)), half = down >> 1;
+                            sum[c][j] = sum[c][j] * power_of_two(half) * power_of_two(down - half);
                         }
                         if (n_ok) retake_sums<16>(sum[c], rows, m0, n, p.x, p.ldx, p.w, p.ldw, p.K);
-                        out.store(p.epi, sum[c], bias, m0, rows, n, n_ok);
+                        // (eight rows of the residual at a time, and after the call: more of them beside the sums went to local
+                        // memory.  3136 x 1024 x 1024 with a residual 45 -> 39 us, without one 45 -> 33)
+                        LinearStore<TYPE, 8> part;
+#pragma unroll
+                        for (int h = 0; h < 16; h += 8) {
+                            float v[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = sum[c][h + j];
+                            part.fetch(p.epi, m0 + h, rows - h, n, n_ok);
+                            part.store(p.epi, v, bias, m0 + h, rows - h, n, n_ok);
+                        }
                     }
             } else {
                 out.fetch(p.epi, m_item + ch0 * 16, rows_at(ch0), n, n_ok);
@@ -292,7 +309,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 }
                 const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * (uint32_t)kPairN;
                 uint32_t v[16];
-                ptx::tmem_ld16(taddr + (uint32_t)(ch0 * 16), v);
+                if (ch0 < ch1) ptx::tmem_ld16(taddr + (uint32_t)(ch0 * 16), v);
                 for (int ch = ch0; ch < ch1; ++ch) {
                     ptx::tmem_ld_wait();
                     float s[16];
@@ -334,7 +351,7 @@ cudaError_t run_pair(PairLinearParams& p, int num_sms, const CUtensorMap (&m)[4]
     p.stages = (kSmem - 1024) / stage_bytes;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     const long long max_pairs = num_sms / 2, pairs = p.items < max_pairs ? p.items : max_pairs;
-    return launch_cluster(2, kern, dim3((unsigned)(2 * pairs)), dim3(kThreads), (size_t)kSmem, stream, m[0], m[1], m[2], m[3], p);
+    return launch_cluster(2, kern, dim3((unsigned)(2 * pairs)), dim3(kThreads<TYPE>), (size_t)kSmem, stream, m[0], m[1], m[2], m[3], p);
 }
 
 }  // namespace
