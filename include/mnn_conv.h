@@ -396,16 +396,17 @@ MNN_API void mnn_net_destroy(mnn_net_t net);
  * activation and residual are evaluated in fp32 and rounded once, at the store.  16-bit operands enter the tensor core as they are,
  * fp32 operands as two halves (hi*hi + lo*hi + hi*lo): TF32 halves, about 21 bits of each value, or, on PAIRS, FP16 halves of rows
  * scaled by a power of two, 24 bits of values down to 2^-16 of their row's largest and 2^-39 of the largest below that.  Relative L2
- * error of fp32 results on normal data: below 1e-6.  An infinity or NaN in x or w gives what the definition gives.  Pointers need the alignment of their element only; x and w on 16-byte boundaries with row strides of a multiple
- * of 16 bytes are read directly, others shifted on the way.  y may be the residual itself (same pointer and stride) and must not
+ * error of fp32 results on normal data: below 1e-6.  An infinity or NaN in x or w gives what the definition gives (slowly in fp32,
+ * where such sums are taken a second time).  Pointers need the alignment of their element only; x and w on 16-byte boundaries with
+ * row strides of a multiple of 16 bytes are read directly, others shifted on the way.  y may be the residual itself (same pointer and stride) and must not
  * overlap x, w or bias.  Nothing is prepared ahead or kept from one run for the next.
  * Rules on pointers, streams and errors as for the convolutions; the current device must be the device of `stream`.
  */
 enum { MNN_TYPE_FP32 = 0, MNN_TYPE_BF16 = 1, MNN_TYPE_FP16 = 2 };
 /* GELU: v (1 + erf(v / sqrt 2)) / 2;  GELU_TANH: v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2;  SILU: v / (1 + e^-v) */
 enum { MNN_ACT_NONE = 0, MNN_ACT_RELU = 1, MNN_ACT_GELU = 2, MNN_ACT_GELU_TANH = 3, MNN_ACT_SILU = 4 };
-/* Kernels: TILES 128 features x 16..256 rows of x on one SM; PAIRS 256 x 128..256 on two; COPIED as TILES for rows that are not 16-byte
- * aligned; FEW up to four rows of x, without tensor cores */
+/* Kernels: TILES 128 features x 16..256 rows of x on one SM; PAIRS 256 x 128..256 on two; COPIED as TILES where only the first row of x or
+ * w is not 16-byte aligned; FEW few rows of x or a small product, without tensor cores */
 enum { MNN_LINEAR_TILES = 0, MNN_LINEAR_PAIRS = 1, MNN_LINEAR_COPIED = 2, MNN_LINEAR_FEW = 3 };
 enum { MNN_RESIDUAL_NONE = 0, MNN_RESIDUAL_AFTER = 1, MNN_RESIDUAL_BEFORE = 2 };
 
@@ -422,13 +423,13 @@ typedef struct {
 typedef struct {
     int M, N, K, type, act, residual;
     int form;                        /* MNN_LINEAR_* for x and w on 16-byte boundaries */
-    int rows_per_item;               /* rows of x per work item */
+    int rows_per_item;               /* rows of x per work item (at most) */
     int features_per_item;
     int split;                       /* CTAs of a cluster (FEW: warps of a CTA) that share an item's K loop */
-    int launches_per_run;            /* 2 where PAIRS lays operands out in the workspace first */
+    int launches_per_run;            /* 2 where operands are laid out in the workspace first */
     int reserved;
     long long items;
-    long long workspace_bytes;       /* the status word, and what PAIRS lays out */
+    long long workspace_bytes;       /* the status word, and the operands laid out anew */
 } mnn_linear_info;
 
 /* Plan one product (host only, needs no GPU); opts may be NULL = fp32, dense, no activation, no residual.  NULL on error:
@@ -464,7 +465,8 @@ MNN_API void mnn_linear_destroy(mnn_linear_plan_t plan);
  *
  * logits [rows][ld] of opts.type, temperature, top_p, min_p, u (float) and top_k (int) are DEVICE arrays of one value per row;
  * each but u may be NULL (temperature 1, nothing cut).  token [rows] int, prob [rows] float or NULL, probs [rows][ld_probs]
- * float or NULL.  Logits are read only; nothing behind a row's last entry is read or written.  One launch, no workspace.
+ * float or NULL.  Logits are read only; nothing behind a row's last entry is read or written.  Outputs must not overlap
+ * inputs or each other.  One launch, no workspace.
  */
 typedef struct mnn_sample_plan_s* mnn_sample_plan_t;   /* opaque host object */
 

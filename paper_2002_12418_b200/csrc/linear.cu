@@ -468,14 +468,19 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     const int eb = f32 ? 4 : 2;
     const bool strides = (s.ldx * eb) % 16 != 0 || (s.ldw * eb) % 16 != 0, copy = unaligned || strides;
     LinearTiling t = {};
-    if (s.M <= 2 || (s.M <= 4 && (long long)s.N * s.K * eb <= 6 << 20)) {
-        // up to four rows: a stream of w (linear_few.cu); two features a warp, and one, and several warps per K loop, where that
-        // leaves fewer than 16 warps per SM.  With three or four rows the sums cost more than the stream once w is large: 4 x 4096 x
-        // 4096 BF16 12.3 us here and 8.4 on tiles, 4 x 1024 x 1000 3.5 and 5.1, two rows 6.9 and 8.2.
+    const long long w_bytes = (long long)s.N * s.K * eb, groups = (s.M + 3) / 4, pairs_of_features = (s.N + 1) / 2;
+    if (s.M <= 2 || (s.M <= 4 && w_bytes <= 6 << 20) ||
+        (groups * pairs_of_features <= 10ll * num_sms && (s.M <= 32 || w_bytes <= 64 << 10) && groups * w_bytes <= (f32 ? 8 : 2) << 20)) {
+        // up to four rows, or several groups of four where the product is small (beyond 32 rows: and w stays in L1): a stream of w (linear_few.cu); two features a warp,
+        // and one, and several warps per K loop, where that leaves fewer than 16 warps per SM.  With three or four rows the sums cost
+        // more than the stream once w is large: 4 x 4096 x 4096 BF16 12.3 us here and 8.4 on tiles, 4 x 1024 x 1000 3.5 and 5.1, two
+        // rows 6.9 and 8.2.  Groups, here and on tiles: fp32 100 x 256 x 48 2.9 and 6.8 us, 100 x 4096 x 16 4.1 and 13.6, 8 x 1024 x 1000 6.8 and
+        // 7.9, 12 x 1024 x 1000 8.8 and 8.0; BF16 100 x 256 x 48 2.5 and 3.5, 6 x 512 x 512 2.9 and 5.1, 8 x 704 x 1472 6.7 and 5.3; and
+        // with many warps 1000 x 64 x 64 7.8 and 3.3 (fp32 6.2 and 5.1).
         t.form = MNN_LINEAR_FEW;
-        t.bm = s.M;
+        t.bm = s.M < 4 ? s.M : 4;
         t.feats = s.M > 2 || s.N / 2 >= 16ll * num_sms ? 2 : 1;
-        t.items = (s.N + t.feats - 1) / t.feats;
+        t.items = (s.N + t.feats - 1) / t.feats * groups;
         t.split = 1;
         while (t.split < 8 && t.items * t.split < 16ll * num_sms && (long long)s.K * eb >= 1024ll * t.split) t.split *= 2;
         return t;
@@ -502,9 +507,9 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         for (int split = 1; split <= 8; split *= 2) {
             // (clusters of eight: only as many as surely run at one time)
             if (split > 1 && (items * split > num_sms || kblocks < 2 * split || (split == 8 && items > 8))) break;
-            const double mma = f32 ? 700.0 + 6.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.form == MNN_LINEAR_COPIED ? 3.0 : 48.0);
+            const double mma = f32 ? 1050.0 + 9.0 * bm : 2.0 * bm, load = (kTileF + bm) * 128.0 / (t.form == MNN_LINEAR_COPIED ? 3.0 : 48.0);
             const long long waves = (items * split + num_sms - 1) / num_sms;
-            const double clocks = waves * ((kblocks + split - 1) / split * (mma > load ? mma : load)) + 1500.0 + 8.0 * bm + (split > 1 ? 1200.0 + 6.0 * bm : 0.0) + tile_relay;
+            const double clocks = waves * ((kblocks + split - 1) / split * (mma > load ? mma : load)) + 1500.0 + (f32 ? 55.0 : 8.0) * bm + (split > 1 ? 1200.0 + 6.0 * bm : 0.0) + tile_relay;
             if (best == 0 || clocks < best) {
                 best = clocks;
                 t.bm = bm;
@@ -514,13 +519,15 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         }
     }
     // Pairs of SMs (linear_pair.cu): half the rows of x per CTA, so that the tensor core and not the delivery decides.  fp32 (as
-    // two FP16 halves, three products) needs a pass over both operands first, as rows that are not aligned do.
-    if (s.M < 192 || t.form == MNN_LINEAR_COPIED) return t;
+    // two FP16 halves, three products) needs a pass over both operands first, as rows that are not aligned do.  Here and on tiles, fp32:
+    // 1024 x 4096 x 1024 66 and 79 us, 1024 x 1024 x 1024 24 and 28, 384 x 2048 x 2048 39 and 43, 512 x 4096 x 1024 (32 items of four
+    // CTAs) 63 and 40; a short K does not earn the pass: 12544 x 128 x 256 19.7 and 13.9.
+    if (s.M < 192 || t.form == MNN_LINEAR_COPIED || (f32 && s.K < 192)) return t;
     const long long blocks = ((long long)s.K + 63) / 64, ld = blocks * 64;
     const double relay = strides || f32 ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
     for (int bm = 256; bm >= 128; bm -= 32) {
         const long long items = ((s.N + 255) / 256) * (long long)((s.M + bm - 1) / bm), pairs = num_sms / 2;
-        const double clocks = (double)((items + pairs - 1) / pairs) * (blocks * (f32 ? 11.0 : 2.6) * bm + (f32 ? 6000.0 : 1000.0)) + 3500.0 + relay;
+        const double clocks = (double)((items + pairs - 1) / pairs) * (blocks * (f32 ? 11.0 : 2.6) * bm + (f32 ? 4000.0 : 1000.0)) + 3500.0 + relay;
         if (clocks < best) {
             best = clocks;
             t.form = MNN_LINEAR_PAIRS;

@@ -95,7 +95,12 @@ struct LinearStore {
 static __device__ __noinline__ float retake_sum(const float* x, const float* w, int K)
 {
     float t = 0.0f;
-    for (int k = 0; k < K; ++k) t = fmaf(x[k], w[k], t);
+    int k = 0;
+    for (; k + 8 <= K && t == t; k += 8) {           // (a NaN stays one)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t = fmaf(x[k + j], w[k + j], t);
+    }
+    for (; k < K && t == t; ++k) t = fmaf(x[k], w[k], t);
     return t;
 }
 template <int NUM>

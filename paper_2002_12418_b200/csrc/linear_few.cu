@@ -1,4 +1,4 @@
-// The matrix product over rows of linear.cu for up to four rows of x: every byte of w is used for a handful of multiply-adds, so
+// The matrix product over rows of linear.cu for groups of up to four rows of x: every byte of w is used for a handful of multiply-adds, so
 // the kernel is a stream of w.  A warp takes two features (one where that leaves too few warps), its lanes 16-byte pieces of both
 // rows of w and of the rows of x (which stay in L1), and sums in fp32; where few features leave too few warps, several warps of a
 // CTA share the K loop and add up in shared memory, in warp order.  No tensor map, barrier pipeline or tensor memory has to be
@@ -55,7 +55,7 @@ template <> struct Wide<MNN_TYPE_FP16> {
     }
 };
 
-// ROWS: rows of x (M is at most that); FEATS: features of a warp; ALIGNED: all rows start on 16-byte boundaries, else their pieces are
+// ROWS: rows of x in a group; FEATS: features of a warp; ALIGNED: all rows start on 16-byte boundaries, else their pieces are
 // shifted together from aligned ones (the second of which the neighbouring lane has brought into L1).
 template <int TYPE, int ROWS, int FEATS, bool ALIGNED>
 __global__ void __launch_bounds__(32 * kWarps)
@@ -70,6 +70,7 @@ linear_few_kernel(FewParams p)
     const int groups = kWarps / p.share;                 // groups of features in this CTA
     const int group = warp / p.share, slice = warp - group * p.share;
     const long long f0 = ((long long)blockIdx.x * groups + group) * FEATS;
+    const int m0 = blockIdx.y * ROWS;                    // first row of x
 
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
@@ -84,7 +85,7 @@ linear_few_kernel(FewParams p)
 #pragma unroll
     for (int f = 0; f < FEATS; ++f) wr[f] = static_cast<const T*>(p.w) + min(f0 + f, (long long)p.N - 1) * p.ldw;
 #pragma unroll
-    for (int m = 0; m < ROWS; ++m) xr[m] = static_cast<const T*>(p.x) + (long long)min(m, p.M - 1) * p.ldx;
+    for (int m = 0; m < ROWS; ++m) xr[m] = static_cast<const T*>(p.x) + (long long)min(m0 + m, p.M - 1) * p.ldx;
     const int pieces = p.K / NUM;
     const int begin = (int)((long long)pieces * slice / p.share), end = (int)((long long)pieces * (slice + 1) / p.share);
     const char *xb = static_cast<const char*>(p.x), *wb = static_cast<const char*>(p.w);
@@ -164,11 +165,11 @@ linear_few_kernel(FewParams p)
     }
     const int m = lane / FEATS;
     const long long n = f0 + (lane - m * FEATS);
-    if (m < p.M && m < ROWS && n < p.N) {
+    if (m0 + m < p.M && m < ROWS && n < p.N) {
         LinearStore<TYPE, 1> out;
-        out.fetch(p.epi, m, 1, (int)n, true);
+        out.fetch(p.epi, m0 + m, 1, (int)n, true);
         float s[1] = {mine};
-        out.store(p.epi, s, linear_bias<TYPE>(p.epi, (int)n, true), m, 1, (int)n, true);
+        out.store(p.epi, s, linear_bias<TYPE>(p.epi, (int)n, true), m0 + m, 1, (int)n, true);
     }
 }
 
@@ -178,7 +179,7 @@ cudaError_t run_rows(const FewParams& p, int feats, bool aligned, cudaStream_t s
     const long long per_cta = (long long)kWarps / p.share * feats, grid = (p.N + per_cta - 1) / per_cta;
     auto kern = feats == 2 ? (aligned ? linear_few_kernel<TYPE, ROWS, 2, true> : linear_few_kernel<TYPE, ROWS, 2, false>)
                            : (aligned ? linear_few_kernel<TYPE, ROWS, 1, true> : linear_few_kernel<TYPE, ROWS, 1, false>);
-    return launch_overlapped(kern, dim3((unsigned)grid), dim3(32 * kWarps), 0, stream, p);
+    return launch_overlapped(kern, dim3((unsigned)grid, (unsigned)((p.M + ROWS - 1) / ROWS)), dim3(32 * kWarps), 0, stream, p);
 }
 
 template <int TYPE>

@@ -188,6 +188,39 @@ def check_infinities(torch, M, K, N, dtype):
     assert r.device_status() == 0
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("M,K,N,pads,offset", [(5, 256, 48, (0, 0, 0, 0), 0), (13, 101, 7, (0, 3, 1, 2), 0), (7, 1000, 77, (0, 0, 0, 0), 1),
+                                               (100, 256, 48, (0, 0, 0, 0), 0), (1001, 40, 1, (0, 0, 0, 0), 0), (5903, 19, 2, (0, 0, 1, 0), 0)])
+def test_groups_of_four_rows(M, K, N, pads, offset, dtype):
+    _, info = run_case(M, K, N, dtype, "silu", "before", pads=pads, offset=offset, seed=M)
+    assert info.form == B.LINEAR_FEW
+
+
+@pytest.mark.parametrize("M,K,N", [(5, 12009, 700), (19, 4099, 530), (200, 4100, 260), (192, 1027, 16), (260, 4099, 300)])
+@pytest.mark.parametrize("dtype", ["fp32", "fp16"])
+def test_operands_laid_out_by_several_warps_a_row(M, K, N, dtype):
+    _, info = run_case(M, K, N, dtype, "none", "after", pads=(1, 0, 0, 0), seed=K)
+    assert info.launches_per_run == 2 or info.form == B.LINEAR_FEW
+
+
+@pytest.mark.parametrize("M,N,form", [(2048, 4096, B.LINEAR_PAIRS), (64, 4096, B.LINEAR_TILES)])
+def test_nothing_but_nan(M, N, form):
+    """Every sum is taken a second time, without a wait that runs out; the workspace is good for the next run."""
+    import torch
+    K = 16384
+    r = B.LinearRunner(M, N, K)
+    assert r.info.form == form
+    x, w = torch.full((M, K), float("nan"), device="cuda"), torch.ones(N, K, device="cuda")
+    y = r.run(x, w)
+    torch.cuda.synchronize()
+    assert r.device_status() == 0 and torch.isnan(y).all()
+    x.fill_(0.5)
+    y = r.run(x, w)
+    torch.cuda.synchronize()
+    assert r.device_status() == 0 and (y == 0.5 * K).all()
+    r.close()
+
+
 def test_relu_keeps_nan_and_half_overflows_to_infinity():
     import torch
     x = torch.full((2, 64), 200.0, dtype=torch.float16, device="cuda")
