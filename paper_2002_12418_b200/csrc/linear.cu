@@ -470,13 +470,14 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     LinearTiling t = {};
     const long long w_bytes = (long long)s.N * s.K * eb, groups = (s.M + 3) / 4, pairs_of_features = (s.N + 1) / 2;
     if (s.M <= 2 || (s.M <= 4 && w_bytes <= 6 << 20) ||
-        (groups * pairs_of_features <= 10ll * num_sms && (s.M <= 32 || w_bytes <= 64 << 10) && groups * w_bytes <= (f32 ? 8 : 2) << 20)) {
-        // up to four rows, or several groups of four where the product is small (beyond 32 rows: and w stays in L1): a stream of w (linear_few.cu); two features a warp,
-        // and one, and several warps per K loop, where that leaves fewer than 16 warps per SM.  With three or four rows the sums cost
-        // more than the stream once w is large: 4 x 4096 x 4096 BF16 12.3 us here and 8.4 on tiles, 4 x 1024 x 1000 3.5 and 5.1, two
-        // rows 6.9 and 8.2.  Groups, here and on tiles: fp32 100 x 256 x 48 2.9 and 6.8 us, 100 x 4096 x 16 4.1 and 13.6, 8 x 1024 x 1000 6.8 and
-        // 7.9, 12 x 1024 x 1000 8.8 and 8.0; BF16 100 x 256 x 48 2.5 and 3.5, 6 x 512 x 512 2.9 and 5.1, 8 x 704 x 1472 6.7 and 5.3; and
-        // with many warps 1000 x 64 x 64 7.8 and 3.3 (fp32 6.2 and 5.1).
+        (groups * pairs_of_features <= 10ll * num_sms && (s.M <= 32 || w_bytes <= 64 << 10) && groups * w_bytes <= (f32 ? strides ? 20 : 8 : 2) << 20)) {
+        // up to four rows, or several groups of four where the product is small (beyond 32 rows: and w stays in L1): a stream of w
+        // (linear_few.cu); two features a warp, and one, and several warps per K loop, where that leaves fewer than 16 warps per SM.
+        // With three or four rows the sums cost more than the stream once w is large: 4 x 4096 x 4096 BF16 12.3 us here and 8.4 on
+        // tiles, 4 x 1024 x 1000 3.5 and 5.1, two rows 6.9 and 8.2.  Groups, here and on tiles: fp32 100 x 256 x 48 2.9 and 6.8 us,
+        // 8 x 1024 x 1000 6.8 and 7.9, 12 x 1024 x 1000 8.8 and 8.0, and 16 x 12009 x 94, which tiles have to lay out first, 20.4 and
+        // 31.9; BF16 100 x 256 x 48 2.5 and 3.5, 6 x 512 x 512 2.9 and 5.1, 8 x 704 x 1472 6.7 and 5.3; and with many warps
+        // 1000 x 64 x 64 7.8 and 3.3 (fp32 6.2 and 5.1).
         t.form = MNN_LINEAR_FEW;
         t.bm = s.M < 4 ? s.M : 4;
         t.feats = s.M > 2 || s.N / 2 >= 16ll * num_sms ? 2 : 1;
