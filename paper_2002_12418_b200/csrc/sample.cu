@@ -439,38 +439,34 @@ sample_kernel(SampleParams p)
     // The first bin at which the running count (or mass) reaches `target`: found by one warp of each CTA, told to all.
     auto cross = [&](bool use_mass, u64 target) {
         if (warp == 0) {
-            u64 base_m = above_mass;
-            uint32_t base_c = above_count, count = 0;
+            // the CTA whose share holds the target
+            const u64 s_m = lane < (int)n_ctas ? ld_cluster(&sh.share_mass, (uint32_t)lane) : 0;
+            const uint32_t s_c = lane < (int)n_ctas ? ld_cluster(&sh.share_count, (uint32_t)lane) : 0;
+            const u64 i_m = above_mass + warp_scan(s_m, lane);
+            const uint32_t i_c = above_count + warp_scan(s_c, lane);
+            const unsigned in = __ballot_sync(0xffffffffu, use_mass ? i_m >= target : (u64)i_c >= target);
+            const int r_lane = in ? __ffs(in) - 1 : 31;
+            u64 base_m = __shfl_sync(0xffffffffu, i_m - s_m, r_lane);
+            uint32_t base_c = __shfl_sync(0xffffffffu, i_c - s_c, r_lane), count = 0;
             int found = -1;
-            for (uint32_t r = 0; r < n_ctas && found < 0; ++r) {
-                const u64 sm = ld_cluster(&sh.share_mass, r);
-                const uint32_t sc = ld_cluster(&sh.share_count, r);
-                if (use_mass ? base_m + sm >= target : (u64)base_c + sc >= target) {
-                    u64 last_m = 0;                                  // of the 32 bins before
-                    uint32_t last_c = 0;
-                    for (int b0 = (int)r * share; found < 0 && b0 < ((int)r + 1) * share; b0 += 32) {
-                        const u64 rm = ld_cluster(&sh.run_mass[b0 + lane], r);
-                        const uint32_t rc = ld_cluster(&sh.run_count[b0 + lane], r);
-                        const unsigned hit = __ballot_sync(0xffffffffu, use_mass ? base_m + rm >= target : (u64)base_c + rc >= target);
-                        if (hit) {
-                            const int src = __ffs(hit) - 1;
-                            const u64 pm = __shfl_sync(0xffffffffu, rm, max(src - 1, 0));
-                            const uint32_t pc = __shfl_sync(0xffffffffu, rc, max(src - 1, 0)), cc = __shfl_sync(0xffffffffu, rc, src);
-                            last_m = src ? pm : last_m;
-                            last_c = src ? pc : last_c;
-                            found = b0 + src;
-                            count = cc - last_c;
-                        } else {
-                            last_m = __shfl_sync(0xffffffffu, rm, 31);
-                            last_c = __shfl_sync(0xffffffffu, rc, 31);
-                        }
-                    }
-                    base_m += last_m;
-                    base_c += last_c;
-                } else {
-                    base_m += sm;
-                    base_c += sc;
-                }
+            if (in) {
+                // every step-th place through the share, then the bins between two of them (a step is at most 32)
+                const uint32_t r = (uint32_t)r_lane;
+                const int b0 = (int)r * share, step = share >> 5;
+                auto first = [&](int at) {
+                    const u64 rm = ld_cluster(&sh.run_mass[b0 + at], r);
+                    const uint32_t rc = ld_cluster(&sh.run_count[b0 + at], r);
+                    const unsigned hit = __ballot_sync(0xffffffffu, use_mass ? base_m + rm >= target : (u64)base_c + rc >= target);
+                    return hit ? __ffs(hit) - 1 : 31;
+                };
+                const int lo = first((lane + 1) * step - 1) * step;
+                const int at = step > 1 ? lo + first(lo + min(lane, step - 1)) : lo;
+                found = b0 + min(at, share - 1);
+                const u64 bm = at ? ld_cluster(&sh.run_mass[found - 1], r) : 0;
+                const uint32_t bc = at ? ld_cluster(&sh.run_count[found - 1], r) : 0;
+                count = ld_cluster(&sh.run_count[found], r) - bc;
+                base_m += bm;
+                base_c += bc;
             }
             if (lane == 0) {
                 sh.found_bin = found;
