@@ -73,6 +73,23 @@ __device__ __forceinline__ u64 ld_cluster(const u64* mine, uint32_t rank)
     return v;
 }
 
+__device__ __forceinline__ void st_cluster(uint32_t* mine, uint32_t v, uint32_t rank)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ptx::map_to_rank(ptx::smem_u32(mine), rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster(u64* mine, u64 v, uint32_t rank)
+{
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(ptx::map_to_rank(ptx::smem_u32(mine), rank)), "l"(v) : "memory");
+}
+// Lane r of a whole warp gives what lane 0 or 31 (`from`) holds to CTA r, in this CTA's place there.  What has few values is given before a
+// barrier and not fetched behind it: a trip to another CTA's shared memory takes some 800 cycles, and a store is not waited for.
+template <typename V>
+__device__ __forceinline__ void give_all(V (&place)[kMaxCtas], V v, int from, uint32_t rank, uint32_t n_ctas, int lane)
+{
+    v = __shfl_sync(0xffffffffu, v, from);
+    if (lane < (int)n_ctas) st_cluster(&place[rank], v, (uint32_t)lane);
+}
+
 // A value that was read from another CTA's shared memory has to be here before this thread arrives at the barrier behind which that
 // memory is written again or its CTA is gone, and a use of it behind the barrier alone does not see to that.  So it decides a
 // branch with a store that is never taken: the largest integer is no mass and no key.
@@ -200,22 +217,23 @@ struct Shared {
     // merged over the cluster: running sums through the bins of this CTA's share
     u64 run_mass[kBins];
     uint32_t run_count[kBins];
-    u64 share_mass;
-    uint32_t share_count;
+    u64 share_mass[kMaxCtas];        // of every CTA
+    uint32_t share_count[kMaxCtas];
     u64 scan_mass[kMaxWarps];
     uint32_t scan_count[kMaxWarps];
     float scan_estimate[kMaxWarps];
-    // sums of the warps' runs and of this CTA
+    // sums of the warps' runs and of the CTAs
     u64 warp_mass[kMaxWarps], warp_above[kMaxWarps];
     uint32_t warp_count[kMaxWarps];
-    u64 cta_mass, cta_above;
-    uint32_t cta_count;
+    u64 cta_whole[kMaxCtas], cta_above[kMaxCtas], cta_mass[kMaxCtas];        // of every CTA
+    uint32_t cta_count[kMaxCtas];
     float warp_max[kMaxWarps];
     float max;                       // of this CTA
     uint32_t key_min, key_max;       // of this CTA
     uint32_t n_list;
     uint32_t list[kGather];          // keys of this CTA's candidates that are to be ranked
-    uint32_t all[kGather];           // of the cluster's
+    uint32_t from_n[kMaxCtas], from[kMaxCtas][kGather];      // of every CTA's
+    uint32_t all[kGather];           // the same in a row
     u64 all_mass[kGather];
     // what one warp found, for all
     uint32_t never;
@@ -429,9 +447,9 @@ sample_kernel(SampleParams p)
                 sh.run_count[b] += base_c;
             }
         }
-        if (threadIdx.x == n_threads - 1) {
-            sh.share_mass = base_m + sum_m;
-            sh.share_count = base_c + sum_c;
+        if (warp == p.n_warps - 1) {                                 // this share's sums, to all
+            give_all(sh.share_mass, base_m + sum_m, 31, rank, n_ctas, lane);
+            give_all(sh.share_count, base_c + sum_c, 31, rank, n_ctas, lane);
         }
         sync_row();                                                  // (all have read this CTA's histograms)
         clear(masses);
@@ -440,8 +458,8 @@ sample_kernel(SampleParams p)
     auto cross = [&](bool use_mass, u64 target) {
         if (warp == 0) {
             // the CTA whose share holds the target
-            const u64 s_m = lane < (int)n_ctas ? ld_cluster(&sh.share_mass, (uint32_t)lane) : 0;
-            const uint32_t s_c = lane < (int)n_ctas ? ld_cluster(&sh.share_count, (uint32_t)lane) : 0;
+            const u64 s_m = lane < (int)n_ctas ? sh.share_mass[lane] : 0;
+            const uint32_t s_c = lane < (int)n_ctas ? sh.share_count[lane] : 0;
             const u64 i_m = above_mass + warp_scan(s_m, lane);
             const uint32_t i_c = above_count + warp_scan(s_c, lane);
             const unsigned in = __ballot_sync(0xffffffffu, use_mass ? i_m >= target : (u64)i_c >= target);
@@ -453,18 +471,23 @@ sample_kernel(SampleParams p)
                 // every step-th place through the share, then the bins between two of them (a step is at most 32)
                 const uint32_t r = (uint32_t)r_lane;
                 const int b0 = (int)r * share, step = share >> 5;
+                u64 bm = 0;                                          // running sums before the first place that reaches the target
+                uint32_t bc = 0, cc = 0;
                 auto first = [&](int at) {
                     const u64 rm = ld_cluster(&sh.run_mass[b0 + at], r);
                     const uint32_t rc = ld_cluster(&sh.run_count[b0 + at], r);
                     const unsigned hit = __ballot_sync(0xffffffffu, use_mass ? base_m + rm >= target : (u64)base_c + rc >= target);
-                    return hit ? __ffs(hit) - 1 : 31;
+                    const int src = hit ? __ffs(hit) - 1 : 31;
+                    const u64 pm = __shfl_sync(0xffffffffu, rm, max(src - 1, 0));
+                    const uint32_t pc = __shfl_sync(0xffffffffu, rc, max(src - 1, 0));
+                    bm = src ? pm : bm;
+                    bc = src ? pc : bc;
+                    cc = __shfl_sync(0xffffffffu, rc, src);
+                    return src;
                 };
                 const int lo = first((lane + 1) * step - 1) * step;
-                const int at = step > 1 ? lo + first(lo + min(lane, step - 1)) : lo;
-                found = b0 + min(at, share - 1);
-                const u64 bm = at ? ld_cluster(&sh.run_mass[found - 1], r) : 0;
-                const uint32_t bc = at ? ld_cluster(&sh.run_count[found - 1], r) : 0;
-                count = ld_cluster(&sh.run_count[found], r) - bc;
+                found = b0 + (step > 1 ? lo + min(first(lo + min(lane, step - 1)), step - 1) : lo);
+                count = cc - bc;
                 base_m += bm;
                 base_c += bc;
             }
@@ -489,10 +512,15 @@ sample_kernel(SampleParams p)
         for_each([&](float l) {
             if (take(l)) sh.list[atomicAdd(&sh.n_list, 1u)] = key(l);
         });
+        __syncthreads();
+        const int mine = (int)sh.n_list;
+        for (int i = threadIdx.x; i < mine * (int)n_ctas; i += n_threads) st_cluster(&sh.from[rank][i / (int)n_ctas], sh.list[i / (int)n_ctas], (uint32_t)(i % (int)n_ctas));
+        if (threadIdx.x < n_ctas) st_cluster(&sh.from_n[rank], (uint32_t)mine, threadIdx.x);
         sync_row();
         u64 sum = 0;
         uint32_t have[kMaxCtas];
-        ld_all(&sh.n_list, n_ctas, have);
+#pragma unroll
+        for (uint32_t c = 0; c < kMaxCtas; ++c) have[c] = c < n_ctas ? sh.from_n[c] : 0;
         for (int at = threadIdx.x; at < n; at += n_threads) {
             int i = at;
             uint32_t r = 0;
@@ -502,7 +530,7 @@ sample_kernel(SampleParams p)
                     i -= (int)have[c];
                     r = c + 1;
                 }
-            const uint32_t k = ld_cluster(&sh.list[i], r);
+            const uint32_t k = sh.from[r][i];
             const u64 w = masses ? weight(value_of_key(k)) : 0;
             sh.all[at] = k;
             sh.all_mass[at] = w;
@@ -512,7 +540,7 @@ sample_kernel(SampleParams p)
             sum = warp_sum(sum);
             if (lane == 0) sh.scan_mass[warp] = sum;
         }
-        sync_row();                                                  // (all have read this CTA's list)
+        __syncthreads();                                             // (before another collection there is a barrier of the cluster)
         if (threadIdx.x == 0) sh.n_list = 0;
         if (masses) {
             sum = 0;
@@ -729,17 +757,17 @@ sample_kernel(SampleParams p)
             __syncthreads();
             if (warp == 0) {
                 const u64 a = warp_sum(lane < p.n_warps ? sh.warp_above[lane] : 0), b = warp_sum(lane < p.n_warps ? sh.warp_mass[lane] : 0);
-                if (lane == 0) {
-                    sh.cta_above = a;
-                    sh.cta_mass = b;
-                }
+                give_all(sh.cta_above, a, 0, rank, n_ctas, lane);
+                give_all(sh.cta_whole, b, 0, rank, n_ctas, lane);
             }
             merge(true);
             u64 whole = 0;
             above_mass = 0;
             above_count = 0;
-            above_mass = sum_all(&sh.cta_above, n_ctas);
-            whole = sum_all(&sh.cta_mass, n_ctas);
+            for (uint32_t r = 0; r < n_ctas; ++r) {
+                above_mass += sh.cta_above[r];
+                whole += sh.cta_whole[r];
+            }
             target = border_target(whole);
             if (above_mass < target) {
                 cross(true, target);
@@ -769,7 +797,8 @@ sample_kernel(SampleParams p)
                 }
             });
             merge(true);
-            u64 whole = sum_all(&sh.share_mass, n_ctas);
+            u64 whole = 0;
+            for (uint32_t r = 0; r < n_ctas; ++r) whole += sh.share_mass[r];
             if (surplus) whole -= surplus * weight(from);
             target = border_target(whole);
             above_mass = 0;
@@ -841,12 +870,10 @@ sample_kernel(SampleParams p)
         run_mass = lane < p.n_warps ? sh.warp_mass[lane] : 0;
         run_count = lane < p.n_warps ? sh.warp_count[lane] : 0;
         const u64 a = warp_sum(run_mass), b = warp_sum(run_count);
-        if (lane == 0) {
-            sh.cta_mass = a;
-            sh.cta_count = (uint32_t)b;
-        }
+        give_all(sh.cta_mass, a, 0, rank, n_ctas, lane);
+        give_all(sh.cta_count, (uint32_t)b, 0, rank, n_ctas, lane);
     }
-    sync_row();
+    sync_row();                                                      // nothing of another CTA is touched behind this: the others may leave
     auto share_of = [&](float l, double per_whole) {                 // weight / kept mass
         const double d = l == m ? 0.0 : (double)l - m_wide;
         return m_inf && l != m ? 0.0f : (float)(exp2_scaled(fmax(d * slope, -1000.0), 1.0, 0) * per_whole);
@@ -855,18 +882,14 @@ sample_kernel(SampleParams p)
     int found_run = -1;
     if (warp == 0) {
         // the CTAs' sums, with as many equals as still count
-        const u64 c_m = lane < (int)n_ctas ? ld_cluster(&sh.cta_mass, (uint32_t)lane) : 0;
-        const u64 c_c = lane < (int)n_ctas ? ld_cluster(&sh.cta_count, (uint32_t)lane) : 0;
+        const u64 c_m = lane < (int)n_ctas ? sh.cta_mass[lane] : 0;
+        const u64 c_c = lane < (int)n_ctas ? sh.cta_count[lane] : 0;
         const u64 cta_seen = warp_scan(c_c, lane) - c_c;
         const u64 c_v = c_m + (cta_seen < ties ? min(c_c, ties - cta_seen) : 0) * border_w;
         const u64 c_incl = warp_scan(c_v, lane);
         total = __shfl_sync(0xffffffffu, c_incl, 31);
         seen0 = __shfl_sync(0xffffffffu, cta_seen, (int)rank);
         before0 = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank);
-        landed(total + c_incl + cta_seen, &sh.never);
-    }
-    sync_row();                                                      // nothing of another CTA is read behind this: the others may leave
-    if (warp == 0) {
         // this CTA's runs
         const u64 seen = seen0 + warp_scan(run_count, lane) - run_count;
         const u64 ties_run = seen < ties ? min(run_count, ties - seen) : 0;
@@ -974,14 +997,14 @@ struct SharedValues {
     float warp_max[kMaxWarps];
     float max;                       // of this CTA
     uint32_t special[2][3];          // planes of the masses of the two shared bins, of this CTA
-    u64 share_mass;
-    uint32_t share_count;
+    u64 share_mass[kMaxCtas];        // of every CTA
+    uint32_t share_count[kMaxCtas];
     u64 scan_mass[kMaxWarps];
     uint32_t scan_count[kMaxWarps];
     u64 warp_mass[kMaxWarps];
     uint32_t warp_count[kMaxWarps];
-    u64 cta_mass;
-    uint32_t cta_count;
+    u64 cta_mass[kMaxCtas];          // of every CTA
+    uint32_t cta_count[kMaxCtas];
     uint32_t key_min, key_max;       // of this CTA
     u64 half_mass;                   // of this CTA, while a range is halved
     uint32_t half_count;
@@ -1194,9 +1217,9 @@ sample_values_kernel(SampleParams p)
                 run_count[at] += base_c;
             }
         }
-        if (threadIdx.x == n_threads - 1) {
-            sh.share_mass = base_m + sum_m;
-            sh.share_count = base_c + sum_c;
+        if (warp == p.n_warps - 1) {                                 // this share's sums, to all
+            give_all(sh.share_mass, base_m + sum_m, 31, rank, n_ctas, lane);
+            give_all(sh.share_count, base_c + sum_c, 31, rank, n_ctas, lane);
         }
         sync_row();
     };
@@ -1204,8 +1227,8 @@ sample_values_kernel(SampleParams p)
     auto cross = [&](bool use_mass, u64 target) {
         if (warp == 0) {
             // the CTA whose share holds the target
-            const u64 s_m = lane < (int)n_ctas ? ld_cluster(&sh.share_mass, (uint32_t)lane) : 0;
-            const uint32_t s_c = lane < (int)n_ctas ? ld_cluster(&sh.share_count, (uint32_t)lane) : 0;
+            const u64 s_m = lane < (int)n_ctas ? sh.share_mass[lane] : 0;
+            const uint32_t s_c = lane < (int)n_ctas ? sh.share_count[lane] : 0;
             const u64 i_m = warp_scan(s_m, lane);
             const uint32_t i_c = warp_scan(s_c, lane);
             const unsigned in = __ballot_sync(0xffffffffu, use_mass ? i_m >= target : (u64)i_c >= target);
@@ -1376,7 +1399,7 @@ sample_values_kernel(SampleParams p)
                 sync_row();
                 whole += ties * weight(from);
             } else {
-                whole = sum_all(&sh.share_mass, n_ctas);
+                for (uint32_t r = 0; r < n_ctas; ++r) whole += sh.share_mass[r];
             }
             // kept while the mass before < p * whole: up to where the running mass reaches ceil(p * whole)
             const u64 target = max(1ull, min((u64)ceil((double)fmaxf(top_p, 0.0f) * (double)whole), whole));
@@ -1445,22 +1468,18 @@ sample_values_kernel(SampleParams p)
     if (warp == 0) {
         const u64 a = warp_sum(lane < p.n_warps ? sh.warp_mass[lane] : 0);
         const uint32_t n = __reduce_add_sync(0xffffffffu, lane < p.n_warps ? sh.warp_count[lane] : 0u);
-        if (lane == 0) {
-            sh.cta_mass = a;
-            sh.cta_count = n;
-        }
+        give_all(sh.cta_mass, a, 0, rank, n_ctas, lane);
+        give_all(sh.cta_count, n, 0, rank, n_ctas, lane);
     }
-    sync_row();
+    sync_row();                                                      // nothing of another CTA is touched behind this: the others may leave
     // every warp: the CTAs' sums, with as many equals as still count
-    const u64 c_m = lane < (int)n_ctas ? ld_cluster(&sh.cta_mass, (uint32_t)lane) : 0;
-    const u64 c_c = lane < (int)n_ctas ? ld_cluster(&sh.cta_count, (uint32_t)lane) : 0;
+    const u64 c_m = lane < (int)n_ctas ? sh.cta_mass[lane] : 0;
+    const u64 c_c = lane < (int)n_ctas ? sh.cta_count[lane] : 0;
     const u64 c_seen = warp_scan(c_c, lane) - c_c;
     const u64 c_v = c_m + (c_seen < ties ? min(c_c, ties - c_seen) : 0) * border_w;
     const u64 c_incl = warp_scan(c_v, lane);
     const u64 total = __shfl_sync(0xffffffffu, c_incl, 31);
     const u64 seen0 = __shfl_sync(0xffffffffu, c_seen, (int)rank), before0 = __shfl_sync(0xffffffffu, c_incl - c_v, (int)rank), mine = __shfl_sync(0xffffffffu, c_v, (int)rank);
-    landed(total + c_incl + c_seen, &sh.never);
-    sync_row();                                                      // nothing of another CTA is read behind this: the others may leave
     const double whole_kept = (double)total, per_whole = (double)unit / whole_kept;
     auto share_of = [&](float l) {                                   // weight / kept mass
         const double d = l == m ? 0.0 : (double)l - m_wide;
