@@ -469,12 +469,17 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     const bool strides = (s.ldx * eb) % 16 != 0 || (s.ldw * eb) % 16 != 0, copy = unaligned || strides;
     LinearTiling t = {};
     const long long w_bytes = (long long)s.N * s.K * eb, groups = (s.M + 3) / 4, pairs_of_features = (s.N + 1) / 2;
-    if (s.M <= 2 || (s.M <= 4 && w_bytes <= 6 << 20) ||
+    // (the most that w may have in bytes for one group of rows)
+    const long long most = s.M <= 2 ? (strides || f32 ? 1ll << 40 : (s.M == 1 ? 64 : 24) << 20) : (f32 ? strides ? 128 : 48 : strides ? 16 : 6) << 20;
+    if ((s.M <= 4 && w_bytes <= most) ||
         (groups * pairs_of_features <= 10ll * num_sms && (s.M <= 32 || w_bytes <= 64 << 10) && groups * w_bytes <= (f32 ? strides ? 20 : 8 : 2) << 20)) {
         // up to four rows, or several groups of four where the product is small (beyond 32 rows: and w stays in L1): a stream of w
         // (linear_few.cu); two features a warp, and one, and several warps per K loop, where that leaves fewer than 16 warps per SM.
-        // With three or four rows the sums cost more than the stream once w is large: 4 x 4096 x 4096 BF16 12.3 us here and 8.4 on
-        // tiles, 4 x 1024 x 1000 3.5 and 5.1, two rows 6.9 and 8.2.  Groups, here and on tiles: fp32 100 x 256 x 48 2.9 and 6.8 us,
+        // The more rows, the sooner the sums cost more than the stream.  Here and on tiles, us: BF16 1 x 2048 x 8192 7.6 and 8.2, 1 x 4096 x
+        // 16384 28.1 and 24.5, 1 x 1008 x 131072 61 and 44, 2 x 1024 x 8192 5.6 and 6.8, 2 x 4096 x 4096 11.7 and 8.3, 4 x 1024 x 1000 3.5 and
+        // 5.1, 4 x 4096 x 4096 12.3 and 8.4; fp32, whose halves cost tiles more, 2 x 2048 x 65536 88 and 131, 4 x 1024 x 8192 8.7 and 14.4,
+        // 4 x 8192 x 8192 81 and 70; rows that tiles have to lay out first: BF16 1 x 1001 x 131072 92 and 155, 2 x 4099 x 16384 53 and 73,
+        // 4 x 1022 x 4314 11.0 and 14.3, 4 x 4097 x 4096 26 and 23, fp32 4 x 1023 x 20000 51 and 69.  Groups: fp32 100 x 256 x 48 2.9 and 6.8,
         // 8 x 1024 x 1000 6.8 and 7.9, 12 x 1024 x 1000 8.8 and 8.0, and 16 x 12009 x 94, which tiles have to lay out first, 20.4 and
         // 31.9; BF16 100 x 256 x 48 2.5 and 3.5, 6 x 512 x 512 2.9 and 5.1, 8 x 704 x 1472 6.7 and 5.3; and with many warps
         // 1000 x 64 x 64 7.8 and 3.3 (fp32 6.2 and 5.1).

@@ -203,6 +203,13 @@ def test_operands_laid_out_by_several_warps_a_row(M, K, N, dtype):
     assert info.launches_per_run == 2 or info.form == B.LINEAR_FEW
 
 
+@pytest.mark.parametrize("dtype,M,K,N,few", [("bf16", 1, 1000, 40000, False), ("fp16", 2, 1024, 14000, False), ("bf16", 2, 1024, 9001, True),
+                                            ("fp32", 4, 1000, 9001, True), ("fp32", 3, 4096, 3100, False), ("fp16", 4, 1022, 5001, True)])
+def test_few_rows_of_large_products(dtype, M, K, N, few):
+    _, info = run_case(M, K, N, dtype, "gelu", "after", seed=N)
+    assert (info.form == B.LINEAR_FEW) == few
+
+
 @pytest.mark.parametrize("M,N,form", [(2048, 4096, B.LINEAR_PAIRS), (64, 4096, B.LINEAR_TILES)])
 def test_nothing_but_nan(M, N, form):
     """Every sum is taken a second time, without a wait that runs out; the workspace is good for the next run."""
