@@ -475,7 +475,7 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         (groups * pairs_of_features <= 10ll * num_sms && (s.M <= 32 || w_bytes <= 64 << 10) && groups * w_bytes <= (f32 ? strides ? 20 : 8 : 2) << 20)) {
         // up to four rows, or several groups of four where the product is small (beyond 32 rows: and w stays in L1): a stream of w
         // (linear_few.cu); two features a warp, and one, and several warps per K loop, where that leaves fewer than 16 warps per SM.
-        // The more rows, the sooner the sums cost more than the stream.  Here and on tiles, us: BF16 1 x 2048 x 8192 7.6 and 8.2, 1 x 4096 x
+        // The more rows, the sooner the sums cost more than the stream.  Here and on tiles, us: BF16 1 x 2048 x 8192 6.2 and 8.2, 1 x 4096 x
         // 16384 28.1 and 24.5, 1 x 1008 x 131072 61 and 44, 2 x 1024 x 8192 5.6 and 6.8, 2 x 4096 x 4096 11.7 and 8.3, 4 x 1024 x 1000 3.5 and
         // 5.1, 4 x 4096 x 4096 12.3 and 8.4; fp32, whose halves cost tiles more, 2 x 2048 x 65536 88 and 131, 4 x 1024 x 8192 8.7 and 14.4,
         // 4 x 8192 x 8192 81 and 70; rows that tiles have to lay out first: BF16 1 x 1001 x 131072 92 and 155, 2 x 4099 x 16384 53 and 73,
