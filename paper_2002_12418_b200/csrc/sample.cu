@@ -48,9 +48,11 @@ constexpr int kMostBytes = 176 * 1024;   // of a row's logits in one CTA: the la
 
 template <int TYPE> struct Logit { typedef float T; static constexpr int kVec = 4; };
 template <> struct Logit<MNN_TYPE_FP16> { typedef __half T; static constexpr int kVec = 8; };
+template <> struct Logit<MNN_TYPE_BF16> { typedef __nv_bfloat16 T; static constexpr int kVec = 8; };
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(__half v) { return __half2float(v); }
+__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
 
 // An integer that orders as the values do.
 __device__ __forceinline__ uint32_t key_of(float v)
@@ -980,7 +982,7 @@ sample_kernel(SampleParams p)
     }
 }
 
-// ---- BF16 rows: by values
+// ---- BF16 rows: by values (long ones of which top-k or top-p may cut something)
 //
 // BF16 logits have few values: below a largest logit of 10, 1568 down to 2^-9.  A bin per value makes counts enough: its mass is
 // the count times one weight, so weights are evaluated once per value and not once per element (the row's passes were bound by
@@ -1647,7 +1649,11 @@ cudaError_t launch_sample(const SampleShape& s, const SampleTiling& t, const Sam
     p.a = a;
     switch (s.type) {
         case MNN_TYPE_FP32: return run_sample<MNN_TYPE_FP32>(s, t, p, stream);
-        case MNN_TYPE_BF16: return run_values(s, t, p, stream);
+        // By values where a border is looked for, in rows of more logits than there are bins.  us, by values and not, top-p 0.9: 512 x 1000
+        // 76.6 and 28.0, 1 x 4000 16.4 and 18.0, 512 x 8000 52.5 and 57.0, 512 x 32000 97 and 124; top-k 300 x 131072 122 and 142 (but 512 x
+        // 32000 81 and 65); neither: 1 x 131072 16.7 and 12.3, 512 x 32000 73 and 49.
+        case MNN_TYPE_BF16:
+            return s.vocab > kValues && (a.top_k || a.top_p) ? run_values(s, t, p, stream) : run_sample<MNN_TYPE_BF16>(s, t, p, stream);
         default: return run_sample<MNN_TYPE_FP16>(s, t, p, stream);
     }
 }

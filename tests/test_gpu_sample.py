@@ -184,6 +184,22 @@ def test_rows_around_zero(dtype):
         check(l, u, **given)
 
 
+# BF16 rows on both sides of the length from which they are cut by values
+@pytest.mark.parametrize("vocab", [300, 4095, 4096, 4097])
+def test_short_bf16_rows(vocab):
+    import torch
+    l, u, g = make(torch, vocab, 12, vocab, "bf16", 1, scale=1.0)
+    l[0:2] -= 20.0
+    l[2:4] *= 1e-3
+    l[4:6] = torch.where(l[4:6].abs() < 1.0, l[4:6] * 1e-4, -l[4:6].abs())
+    l[6:8] = l[6:8].round()
+    l[8, ::3], l[9, 5], l[10] = float("-inf"), float("nan"), float("-inf")
+    p = torch.rand(12, generator=g, device="cuda")
+    k = torch.randint(0, vocab + 2, (12,), generator=g, device="cuda", dtype=torch.int32)
+    for given in ({}, dict(top_k=k), dict(top_p=p), dict(top_k=k, top_p=p), dict(min_p=p), dict(top_p=p, min_p=p * 0.1), dict(temperature=p * 1e-3, top_p=p)):
+        check(l, u, **given)
+
+
 # the draws follow the distribution: 20000 equal rows, the frequency of each token within 6 standard deviations
 def test_draws_follow_the_distribution():
     import torch
