@@ -203,6 +203,12 @@ def test_operands_laid_out_by_several_warps_a_row(M, K, N, dtype):
     assert info.launches_per_run == 2 or info.form == B.LINEAR_FEW
 
 
+@pytest.mark.parametrize("M,K,N,pads", [(80, 1001, 8000, (0, 0, 0, 0)), (114, 707, 6225, (0, 2, 1, 0))])
+def test_pairs_of_fewer_unaligned_rows(M, K, N, pads):
+    _, info = run_case(M, K, N, "fp32", "relu", "before", pads=pads, seed=M)
+    assert info.form == B.LINEAR_PAIRS
+
+
 @pytest.mark.parametrize("dtype,M,K,N,few", [("bf16", 1, 1000, 40000, False), ("fp16", 2, 1024, 14000, False), ("bf16", 2, 1024, 9001, True),
                                             ("fp32", 4, 1000, 9001, True), ("fp32", 3, 4096, 3100, False), ("fp16", 4, 1022, 5001, True)])
 def test_few_rows_of_large_products(dtype, M, K, N, few):
