@@ -529,11 +529,12 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     // 1024 x 4096 x 1024 66 and 79 us, 1024 x 1024 x 1024 24 and 28, 384 x 2048 x 2048 39 and 43, 512 x 4096 x 1024 (32 items of four
     // CTAs) 63 and 40; a short K does not earn the pass: 12544 x 128 x 256 19.7 and 13.9.
     // Fewer rows only where tiles have to lay fp32 operands out as well: 80 x 1001 x 8000 39 and 45, but 128 x 1024 x 32000 98 and 76.
-    if (s.M < (f32 && strides ? 72 : 192) || t.form == MNN_LINEAR_COPIED || (f32 && s.K < 192)) return t;
+    const long long pairs = num_sms / 2;
+    if (s.M < (f32 && strides ? 72 : 192) || t.form == MNN_LINEAR_COPIED || (f32 && s.K < 192) || pairs < 1) return t;
     const long long blocks = ((long long)s.K + 63) / 64, ld = blocks * 64;
     const double relay = strides || f32 ? 3000.0 + 2.0 * operand_bytes / (20.0 * num_sms) : 0.0;
     for (int bm = 256; bm >= 128; bm -= 32) {
-        const long long items = ((s.N + 255) / 256) * (long long)((s.M + bm - 1) / bm), pairs = num_sms / 2;
+        const long long items = ((s.N + 255) / 256) * (long long)((s.M + bm - 1) / bm);
         const double clocks = (double)((items + pairs - 1) / pairs) * (blocks * (f32 ? 11.0 : 2.6) * bm + (f32 ? 4000.0 : 1000.0)) + 3500.0 + relay;
         if (clocks < best) {
             best = clocks;

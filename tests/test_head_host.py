@@ -1,12 +1,15 @@
 """Host-side checks of the matrix product over rows and of sampling: arguments that are refused, what a plan decides, and the
 oracle on cases worked by hand.  No GPU."""
 import ctypes
+import subprocess
+import sys
 
 import numpy as np
 import pytest
 
 from oracle import rows as oracle
 from paper_2002_12418_b200 import binding as B
+from tests.conftest import ROOT
 
 
 def linear(*a, **kw):
@@ -83,6 +86,26 @@ def test_linear_plans():
                     assert i.features_per_item == (256 if i.form == B.LINEAR_PAIRS else 128)
                     assert i.items == -(-N // i.features_per_item) * -(-M // i.rows_per_item) and i.rows_per_item <= 256
                 assert i.split in (1, 2, 4, 8)
+
+
+# the record's number of SMs may be any positive number: plans on one SM have no pairs.  (In a process of their own: this once ended it.)
+@pytest.mark.parametrize("sms", [1, 2, 3, 148, 100000])
+def test_plans_for_any_number_of_sms(sms):
+    code = """
+from paper_2002_12418_b200 import binding as B
+c = B.mnn_get_calibration()
+c[7] = %d
+B.mnn_set_calibration(c)
+for dtype in B.TYPES:
+    for M, N, K in ((1, 64, 64), (192, 4096, 4096), (300, 300, 301), (5000, 700, 1024)):
+        p = B.mnn_linear_plan(M, N, K, B.make_linear_opts(dtype))
+        i = B.mnn_linear_plan_query(p)
+        assert i.items > 0 and (%d > 1 or i.form != B.LINEAR_PAIRS), (dtype, M, N, K)
+        B.mnn_linear_destroy(p)
+    B.mnn_sample_destroy(B.mnn_sample_plan(64, 32000, B.make_sample_opts(dtype)))
+""" % (sms, sms)
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, (r.returncode, r.stderr)
 
 
 def test_sample_refusals():
