@@ -1053,6 +1053,7 @@ int mnn_set_calibration(const long long consts[MNN_N_CONSTS])
     for (int i = 0; i < MNN_N_CONSTS; ++i) c.c[i] = consts[i];
     for (int i = 0; i <= 8; ++i)
         if (c.c[i] <= 0) return fail(MNN_EINVAL, "constants 0..8 must be positive");
+    if (c.c[7] > (1 << 20)) return fail(MNN_EINVAL, "constant 7 (SMs) must be at most 2^20");
     install_calibration(c);
     return MNN_OK;
 }

@@ -108,6 +108,26 @@ for dtype in B.TYPES:
     assert r.returncode == 0, (r.returncode, r.stderr)
 
 
+# numbers of SMs that a plan's integers cannot hold are refused, and the record in force stays
+@pytest.mark.parametrize("sms", [0, -1, (1 << 20) + 1, 1 << 32, (1 << 32) + 1, (1 << 31) + 5])
+def test_numbers_of_sms_that_are_refused(sms):
+    code = """
+from paper_2002_12418_b200 import binding as B
+before = B.mnn_get_calibration()
+c = list(before)
+c[7] = %d
+try:
+    B.mnn_set_calibration(c)
+    said = "taken"
+except B.MnnError as e:
+    said = e.code
+B.mnn_linear_plan(192, 4096, 4096, B.make_linear_opts("bf16"))
+assert said == B.MNN_EINVAL and B.mnn_get_calibration() == before, said
+""" % sms
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, (r.returncode, r.stderr)
+
+
 def test_sample_refusals():
     for shape, kw in (((0, 5), {}), ((5, 0), {}), ((2, 10), dict(ld=9)), ((2, 10), dict(ld_probs=9)), ((2, B.SAMPLE_MAX_VOCAB + 1), {}),
                       ((1 << 28, 10), {}), ((2, 10), dict(dtype="fp64")), ((2, 10), dict(ld=1 << 40))):
