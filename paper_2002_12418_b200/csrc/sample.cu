@@ -99,6 +99,13 @@ __device__ __forceinline__ void landed(u64 v, uint32_t* never)
 {
     if (v == ~0ull) *reinterpret_cast<volatile uint32_t*>(never) = 1;
 }
+// The same for what a row was given, by one sum of all of it.  (Whatever the values are: nothing reads what is stored.)  In a row without a
+// candidate nothing else asks for these values before the last barrier.
+__device__ __forceinline__ void landed(float temperature, float top_p, float min_p, float u, int top_k, uint32_t* never)
+{
+    const uint32_t sum = __float_as_uint(temperature) + __float_as_uint(top_p) + __float_as_uint(min_p) + __float_as_uint(u) + (uint32_t)top_k;
+    if (sum == ~0u) *reinterpret_cast<volatile uint32_t*>(never) = 1;
+}
 
 // One value of every CTA, all reads in flight together; 0 for CTAs that are not there.
 template <typename V>
@@ -349,6 +356,7 @@ sample_kernel(SampleParams p)
     const float temperature = ld_cluster_float(&sh.row.temperature), top_p = ld_cluster_float(&sh.row.top_p), min_p = ld_cluster_float(&sh.row.min_p);
     const int top_k = (int)ld_cluster(reinterpret_cast<const uint32_t*>(&sh.row.top_k), 0);
     const float u_row = ld_cluster_float(&sh.row.u);
+    landed(temperature, top_p, min_p, u_row, top_k, &sh.never);
     const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
     const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
     const bool some = m > -INFINITY;
@@ -1114,6 +1122,7 @@ sample_values_kernel(SampleParams p)
     const float temperature = ld_cluster_float(&sh.row.temperature), top_p = ld_cluster_float(&sh.row.top_p), min_p = ld_cluster_float(&sh.row.min_p);
     const int top_k = (int)ld_cluster(reinterpret_cast<const uint32_t*>(&sh.row.top_k), 0);
     const float u_row = ld_cluster_float(&sh.row.u);
+    landed(temperature, top_p, min_p, u_row, top_k, &sh.never);
     const bool one = !(temperature > 0.0f) || top_k == 1;            // the first largest alone
     const bool by_count = !one && top_k > 0 && top_k < p.vocab, by_mass = !one && top_p < 1.0f;
     const bool some = m > -INFINITY;

@@ -117,6 +117,33 @@ def test_masks(vocab, dtype):
         assert token[0] == -1 and token[1] == -1 and token[3] == 0
 
 
+# long rows of which nothing is left, in clusters, whatever they were given: nothing in the kernel needs these values before its last barrier
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [20000, 200001])
+def test_rows_of_nothing(vocab, dtype):
+    import torch
+    rows = 64
+    l = torch.full((rows, vocab), float("-inf"), device="cuda").to(types(torch)[dtype])
+    l[1::3] = float("nan")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    given = {k: torch.rand(rows, generator=g, device="cuda") for k in ("temperature", "top_p", "min_p")}
+    u = torch.rand(rows, generator=g, device="cuda")
+    k = torch.randint(0, 300, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    given["temperature"][0:2], k[0:4] = float("nan"), -1
+    for t in (given["top_p"], u):
+        t.view(torch.int32)[2:4] = -1                # a NaN of nothing but ones
+    r = B.SampleRunner(rows, vocab, dtype)
+    assert vocab < 100000 or r.info.ctas_per_row > 1
+    for _ in range(20):
+        token, prob, dist = r.run(l, u, top_k=k, probs=True, **given)
+        assert (token == -1).all() and (prob == 0).all() and (dist == 0).all()
+    # and a draw from the last value alone
+    l[:, -1] = 1.0
+    token, prob, dist = r.run(l, u, top_k=k, probs=True, **given)
+    assert (token == vocab - 1).all() and (prob == 1).all() and (dist[:, -1] == 1).all() and (dist[:, :-1] == 0).all()
+
+
 # values that tie by the thousand: the first ones by index stay
 @pytest.mark.parametrize("vocab", [100, 20011])
 @pytest.mark.parametrize("levels", [1, 2, 5])
