@@ -462,7 +462,30 @@ def _raw_stream(device):
     return lambda: raw(index)
 
 
-class NetRunner:
+class _OwnsWorkspace:
+    """A runner's workspace, from torch's allocator.  The allocator gives memory that was freed to the next taker on the stream that it
+    was allocated on, so it has to know of the other streams that use it: each is recorded at its first run.  A runner may then
+    be dropped behind a run on any stream.  (A captured graph is no stream: the runners whose runs it holds have to outlive it.)"""
+    workspace = None
+
+    def _allocate_workspace(self, nbytes: int, hand_over) -> None:
+        torch = self.torch
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(nbytes + 1024, dtype=torch.uint8, device=self.device)
+            self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
+            self._ws_streams = {self._raw_stream()}
+            hand_over(self._ws_ptr, nbytes)
+
+    def stream(self) -> int:
+        """The handle of torch's current stream, which is about to use the workspace."""
+        handle = self._raw_stream()
+        if self.workspace is not None and handle not in self._ws_streams:
+            self._ws_streams.add(handle)
+            self.workspace.record_stream(self.torch.cuda.current_stream(self.device))
+        return handle
+
+
+class NetRunner(_OwnsWorkspace):
     """A network plan plus its torch-owned workspace; ``run`` is one mnn_net_run on torch's current stream."""
 
     def __init__(self, N, H, W, layers, precision=PREC_TF32, device="cuda:0"):
@@ -472,14 +495,8 @@ class NetRunner:
         self._raw_stream = _raw_stream(self.device)
         self.net = mnn_net_plan(N, H, W, layers, precision)
         self.info = mnn_net_query(self.net)
-        with torch.cuda.device(self.device):
-            self.workspace = torch.empty(self.info.workspace_bytes + 1024, dtype=torch.uint8, device=self.device)
-        self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
-        mnn_net_set_workspace(self.net, self._ws_ptr, self.info.workspace_bytes)
+        self._allocate_workspace(self.info.workspace_bytes, lambda ptr, nbytes: mnn_net_set_workspace(self.net, ptr, nbytes))
         self._keep = None
-
-    def stream(self) -> int:
-        return self._raw_stream()
 
     def prepare(self, ws) -> None:
         mnn_net_prepare(self.net, [w.data_ptr() for w in ws], self.stream())
@@ -511,7 +528,7 @@ class NetRunner:
             pass
 
 
-class ConvLayerRunner:
+class ConvLayerRunner(_OwnsWorkspace):
     """A plan plus its torch-owned workspace.  ``run`` launches on torch's current
     stream through mnn_conv_run; nothing here computes."""
 
@@ -528,16 +545,8 @@ class ConvLayerRunner:
             self.plan = mnn_conv_plan_ex(N, Cin, Cout, H, W, k, stride, pad, dilation, opts) if opts is not None \
                 else mnn_conv_plan(N, Cin, Cout, H, W, k, stride, pad, dilation)
         self.info = mnn_conv_plan_query(self.plan)
-        self.workspace = None
         if self.info.workspace_bytes > 0:
-            with torch.cuda.device(self.device):
-                self.workspace = torch.empty(self.info.workspace_bytes + 1024, dtype=torch.uint8, device=self.device)
-                base = self.workspace.data_ptr()
-                self._ws_ptr = (base + 1023) // 1024 * 1024
-                mnn_conv_set_workspace(self.plan, self._ws_ptr, self.info.workspace_bytes)
-
-    def stream(self) -> int:
-        return self._raw_stream()
+            self._allocate_workspace(self.info.workspace_bytes, lambda ptr, nbytes: mnn_conv_set_workspace(self.plan, ptr, nbytes))
 
     def prepare(self, w) -> None:
         mnn_conv_prepare_weights(self.plan, w.data_ptr(), self.stream())
@@ -612,10 +621,10 @@ class _RowRunner:
         """The library's call with this runner's device as the current one."""
         torch = self.torch
         if torch._C._cuda_getDevice() == self.device.index:
-            rc = call(self.plan, *args, self._raw_stream())
+            rc = call(self.plan, *args, self.stream())
         else:
             with torch.cuda.device(self.device):
-                rc = call(self.plan, *args, self._raw_stream())
+                rc = call(self.plan, *args, self.stream())
         if rc != MNN_OK:
             _check(rc)
 
@@ -626,7 +635,7 @@ class _RowRunner:
             pass
 
 
-class LinearRunner(_RowRunner):
+class LinearRunner(_OwnsWorkspace, _RowRunner):
     """y = act(x w^T + bias) with a residual (``mnn_linear_plan`` / ``mnn_linear_run``): x [M, K], w [N, K], bias [N],
     residual and y [M, N], all of one type ("fp32", "bf16", "fp16").  Row strides that differ from dense ones are planned
     (ldx, ldw, ldy, ldr)."""
@@ -639,10 +648,7 @@ class LinearRunner(_RowRunner):
         self._M, self._N, self._ld_y = M, N, ldy or N
         self._x, self._w, self._y, self._n = torch.Size((M, K)), torch.Size((N, K)), torch.Size((M, N)), torch.Size((N,))
         self._sx, self._sw, self._sy, self._sr = (ldx or K, 1), (ldw or K, 1), (ldy or N, 1), (ldr or N, 1)
-        with torch.cuda.device(self.device):
-            self.workspace = torch.empty(self.info.workspace_bytes + 1024, dtype=torch.uint8, device=self.device)
-            self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
-            mnn_linear_set_workspace(self.plan, self._ws_ptr, self.info.workspace_bytes)
+        self._allocate_workspace(self.info.workspace_bytes, lambda ptr, nbytes: mnn_linear_set_workspace(self.plan, ptr, nbytes))
 
     def run(self, x, w, bias=None, residual=None, y=None):
         dtype = self.dtype

@@ -185,3 +185,55 @@ def test_oracle_linear_by_hand():
     assert abs(oracle.activate(np.array(1.0), "gelu") - 0.8413447460685429) < 1e-15
     assert abs(oracle.activate(np.array(1.0), "gelu_tanh") - 0.8411919906082768) < 1e-15
     assert abs(oracle.activate(np.array(1.0), "silu") - 0.7310585786300049) < 1e-15
+
+
+class _FakeTorch:
+    """A current stream that a test sets, and tensors that remember the streams recorded on them."""
+    uint8 = None
+
+    def __init__(self):
+        self.cuda, self.now, self.recorded = self, 0, []
+
+    def device(self, _):
+        import contextlib
+        return contextlib.nullcontext()
+
+    def empty(self, *_, **__):
+        return self
+
+    def data_ptr(self):
+        return 5000
+
+    def current_stream(self, _):
+        return "stream %d" % self.now
+
+    def record_stream(self, stream):
+        self.recorded.append(stream)
+
+
+@pytest.mark.parametrize("runner", [B.LinearRunner, B.ConvLayerRunner, B.NetRunner])
+def test_streams_that_use_a_workspace_are_recorded(runner):
+    torch = _FakeTorch()
+    r = runner.__new__(runner)
+    r.torch, r.device, r._raw_stream = torch, None, lambda: torch.now
+    assert r.stream() == 0 and torch.recorded == []         # nothing to record yet
+    torch.now, given = 3, []
+    r._allocate_workspace(4096, lambda *a: given.append(a))
+    assert given == [(5120, 4096)]
+    for now in (3, 3, 7, 7, 0, 3, 7, 0):
+        torch.now = now
+        assert r.stream() == now
+    assert torch.recorded == ["stream 7", "stream 0"]
+
+
+def test_a_run_over_rows_asks_for_its_stream_through_the_workspace():
+    import types
+    torch = _FakeTorch()
+    torch._C = types.SimpleNamespace(_cuda_getDevice=lambda: 0)
+    r = B.LinearRunner.__new__(B.LinearRunner)
+    r.torch, r.device, r.plan, r._raw_stream = torch, types.SimpleNamespace(index=0), None, lambda: torch.now
+    r._allocate_workspace(4096, lambda *a: None)
+    torch.now = 9
+    calls = []
+    r._launch(lambda *a: calls.append(a) or B.MNN_OK, 1, 2)
+    assert calls == [(None, 1, 2, 9)] and torch.recorded == ["stream 9"]
