@@ -473,15 +473,20 @@ class _OwnsWorkspace:
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(nbytes + 1024, dtype=torch.uint8, device=self.device)
             self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
-            self._ws_streams = {self._raw_stream()}
+            self._ws_streams = {self._raw_stream() if self.workspace.is_cuda else 0}
             hand_over(self._ws_ptr, nbytes)
 
     def stream(self) -> int:
-        """The handle of torch's current stream, which is about to use the workspace."""
-        handle = self._raw_stream()
+        """The stream of the runs (torch's current one; a subclass may choose)."""
+        return self._raw_stream()
+
+    def _run_stream(self) -> int:
+        """The handle of the stream that is about to use the workspace."""
+        handle = self.stream()
         if self.workspace is not None and handle not in self._ws_streams:
             self._ws_streams.add(handle)
-            self.workspace.record_stream(self.torch.cuda.current_stream(self.device))
+            if self.workspace.is_cuda:
+                self.workspace.record_stream(self.torch.cuda.ExternalStream(handle, device=self.device))
         return handle
 
 
@@ -499,7 +504,7 @@ class NetRunner(_OwnsWorkspace):
         self._keep = None
 
     def prepare(self, ws) -> None:
-        mnn_net_prepare(self.net, [w.data_ptr() for w in ws], self.stream())
+        mnn_net_prepare(self.net, [w.data_ptr() for w in ws], self._run_stream())
 
     def bind(self, ws, bs) -> None:
         """Marshal the weight / bias pointer arrays once (they are reused by every run)."""
@@ -510,7 +515,7 @@ class NetRunner(_OwnsWorkspace):
         if y is None:
             y = torch.empty((self.info.N, self.info.out_C, self.info.out_H, self.info.out_W), dtype=torch.float32,
                             device=self.device)
-        _check(lib().mnn_net_run(self.net, x.data_ptr(), self._keep[0], self._keep[1], y.data_ptr(), self.stream()))
+        _check(lib().mnn_net_run(self.net, x.data_ptr(), self._keep[0], self._keep[1], y.data_ptr(), self._run_stream()))
         return y
 
     def device_status(self):
@@ -549,19 +554,19 @@ class ConvLayerRunner(_OwnsWorkspace):
             self._allocate_workspace(self.info.workspace_bytes, lambda ptr, nbytes: mnn_conv_set_workspace(self.plan, ptr, nbytes))
 
     def prepare(self, w) -> None:
-        mnn_conv_prepare_weights(self.plan, w.data_ptr(), self.stream())
+        mnn_conv_prepare_weights(self.plan, w.data_ptr(), self._run_stream())
 
     def run(self, x, w, bias=None, y=None, stage_mask=None):
         if y is None:
             y = self.torch.empty((self.shape[0], self.shape[2], self.info.OH, self.info.OW), dtype=self.torch.float32, device=self.device)
         bp = bias.data_ptr() if bias is not None else None
         if stage_mask is None:
-            rc = _lib.mnn_conv_run(self.plan, x.data_ptr(), w.data_ptr(), bp, y.data_ptr(), self.stream())
+            rc = _lib.mnn_conv_run(self.plan, x.data_ptr(), w.data_ptr(), bp, y.data_ptr(), self._run_stream())
             if rc != MNN_OK:
                 _check(rc)
         else:
             mnn_conv_run_stages(self.plan, x.data_ptr() if x is not None else None,
-                                w.data_ptr() if w is not None else None, bp, y.data_ptr(), self.stream(), stage_mask)
+                                w.data_ptr() if w is not None else None, bp, y.data_ptr(), self._run_stream(), stage_mask)
         return y
 
     def workspace_view(self, offset: int, nbytes: int, dtype):
@@ -602,6 +607,9 @@ class _RowRunner:
     def stream(self) -> int:
         return self._raw_stream()
 
+    def _run_stream(self) -> int:
+        return self.stream()
+
     def _rows(self, t, shape, strides, what, dtype):
         """The address of a tensor of `shape` whose rows lie as `strides` says."""
         if t.dtype is not dtype or t.device != self.device or t.shape != shape:
@@ -621,10 +629,10 @@ class _RowRunner:
         """The library's call with this runner's device as the current one."""
         torch = self.torch
         if torch._C._cuda_getDevice() == self.device.index:
-            rc = call(self.plan, *args, self.stream())
+            rc = call(self.plan, *args, self._run_stream())
         else:
             with torch.cuda.device(self.device):
-                rc = call(self.plan, *args, self.stream())
+                rc = call(self.plan, *args, self._run_stream())
         if rc != MNN_OK:
             _check(rc)
 

@@ -55,3 +55,30 @@ def test_memory_of_a_dropped_runner_waits_for_its_run(make):
     assert all(t.data_ptr() != at for t in taken)
     torch.cuda.synchronize()
     assert torch.allclose(y, torch.full_like(y, want), rtol=1e-3)
+
+
+def test_a_subclass_s_stream_is_recorded():
+    import torch
+    side = torch.cuda.Stream()
+
+    class OnSide(B.LinearRunner):
+        def stream(self):
+            return side.cuda_stream
+
+    x, w, y = torch.ones(1500, 640, device="cuda"), torch.ones(1300, 640, device="cuda"), torch.empty(1500, 1300, device="cuda")
+    r = OnSide(1500, 1300, 640)
+    size, at = r.workspace.numel(), r.workspace.data_ptr()
+    torch.cuda.synchronize()
+    r.run(x, w, y=y)
+    torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255)
+    torch.cuda.synchronize()
+    y.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)
+    r.run(x, w, y=y)
+    del r
+    taken = [torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255) for _ in range(2)]
+    assert not side.query() and all(t.data_ptr() != at for t in taken)
+    torch.cuda.synchronize()
+    assert (y == 640).all()

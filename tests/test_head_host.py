@@ -189,7 +189,7 @@ def test_oracle_linear_by_hand():
 
 class _FakeTorch:
     """A current stream that a test sets, and tensors that remember the streams recorded on them."""
-    uint8 = None
+    uint8, is_cuda = None, True
 
     def __init__(self):
         self.cuda, self.now, self.recorded = self, 0, []
@@ -204,8 +204,8 @@ class _FakeTorch:
     def data_ptr(self):
         return 5000
 
-    def current_stream(self, _):
-        return "stream %d" % self.now
+    def ExternalStream(self, handle, device):
+        return "stream %d" % handle
 
     def record_stream(self, stream):
         self.recorded.append(stream)
@@ -216,14 +216,16 @@ def test_streams_that_use_a_workspace_are_recorded(runner):
     torch = _FakeTorch()
     r = runner.__new__(runner)
     r.torch, r.device, r._raw_stream = torch, None, lambda: torch.now
-    assert r.stream() == 0 and torch.recorded == []         # nothing to record yet
-    torch.now, given = 3, []
+    assert r._run_stream() == 0 and torch.recorded == []    # nothing to record yet
+    torch.now, given = 0, []
     r._allocate_workspace(4096, lambda *a: given.append(a))
     assert given == [(5120, 4096)]
-    for now in (3, 3, 7, 7, 0, 3, 7, 0):
+    for now in (0, 0, 7, 7, 3, 0, 7, 3):
         torch.now = now
-        assert r.stream() == now
-    assert torch.recorded == ["stream 7", "stream 0"]
+        assert r._run_stream() == now
+    assert torch.recorded == ["stream 7", "stream 3"]
+    r.stream = lambda: 11                                   # as a subclass's that chooses the stream
+    assert r._run_stream() == 11 and torch.recorded[2:] == ["stream 11"]
 
 
 def test_a_run_over_rows_asks_for_its_stream_through_the_workspace():
@@ -232,8 +234,7 @@ def test_a_run_over_rows_asks_for_its_stream_through_the_workspace():
     torch._C = types.SimpleNamespace(_cuda_getDevice=lambda: 0)
     r = B.LinearRunner.__new__(B.LinearRunner)
     r.torch, r.device, r.plan, r._raw_stream = torch, types.SimpleNamespace(index=0), None, lambda: torch.now
-    r._allocate_workspace(4096, lambda *a: None)
-    torch.now = 9
-    calls = []
+    r._allocate_workspace(4096, lambda *a: None)            # on the default stream
+    torch.now, calls = 9, []
     r._launch(lambda *a: calls.append(a) or B.MNN_OK, 1, 2)
     assert calls == [(None, 1, 2, 9)] and torch.recorded == ["stream 9"]
