@@ -209,7 +209,10 @@ MNN_API int mnn_conv_plan_query(mnn_conv_plan_t plan, mnn_conv_info* info);
 /* Hand the plan its device workspace (>= info.workspace_bytes, 1024-byte aligned).
  * The caller keeps ownership and must keep it alive while the plan is used
  * (memory pre-allocation ahead of inference, Section 3.2 "preparation-execution
- * decoupling").  Invalidates prepared weights. */
+ * decoupling").  Invalidates prepared weights.  The status word is cleared on the
+ * legacy default stream: whatever else uses the memory has to be over, and runs on
+ * a stream that does not wait for that one (a non-blocking stream) have to be
+ * ordered behind it by the caller.  The same holds for the other _set_workspace. */
 MNN_API int mnn_conv_set_workspace(mnn_conv_plan_t plan, void* workspace, long long bytes);
 
 /* Transform the weights into the workspace now (U = G w G^T of Eq. 6, or the

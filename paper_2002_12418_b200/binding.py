@@ -473,8 +473,14 @@ class _OwnsWorkspace:
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(nbytes + 1024, dtype=torch.uint8, device=self.device)
             self._ws_ptr = (self.workspace.data_ptr() + 1023) // 1024 * 1024
-            self._ws_streams = {self._raw_stream() if self.workspace.is_cuda else 0}
+            home = self._raw_stream() if self.workspace.is_cuda else 0
+            self._ws_streams = {home}
+            # the library clears a word of it on the default stream, which another one does not wait for (nor it for that one)
+            if home:
+                torch.cuda.current_stream(self.device).synchronize()
             hand_over(self._ws_ptr, nbytes)
+            if home:
+                torch.cuda.default_stream(self.device).synchronize()
 
     def stream(self) -> int:
         """The stream of the runs (torch's current one; a subclass may choose)."""

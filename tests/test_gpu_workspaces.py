@@ -57,6 +57,29 @@ def test_memory_of_a_dropped_runner_waits_for_its_run(make):
     assert torch.allclose(y, torch.full_like(y, want), rtol=1e-3)
 
 
+def test_a_runner_built_on_a_stream_leaves_its_memory_s_last_user_alone():
+    import torch
+    r = B.LinearRunner(4, 8, 16)
+    size = r.workspace.numel()
+    x, w = torch.ones(4, 16, device="cuda"), torch.ones(8, 16, device="cuda")
+    r.run(x, w)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.empty(size, dtype=torch.uint8, device="cuda").fill_(77).clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        first = torch.empty(size, dtype=torch.uint8, device="cuda").fill_(77)
+        at = first.data_ptr()
+        torch.cuda._sleep(200_000_000)
+        copy = first.clone()
+        del first
+        r2 = B.LinearRunner(4, 8, 16)                # takes the memory that `first` had, which the copy has not read yet
+        assert r2.workspace.data_ptr() == at
+        y = r2.run(x, w)
+    torch.cuda.synchronize()
+    assert (copy == 77).all() and (y == 16).all() and r2.device_status() == 0
+
+
 def test_a_subclass_s_stream_is_recorded():
     import torch
     side = torch.cuda.Stream()

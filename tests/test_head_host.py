@@ -238,3 +238,18 @@ def test_a_run_over_rows_asks_for_its_stream_through_the_workspace():
     torch.now, calls = 9, []
     r._launch(lambda *a: calls.append(a) or B.MNN_OK, 1, 2)
     assert calls == [(None, 1, 2, 9)] and torch.recorded == ["stream 9"]
+
+
+# handing memory over clears a word of it on the default stream: with a runner built on another stream, nothing may still be using the
+# memory there, and the clearing has to be over before that stream goes on
+@pytest.mark.parametrize("home,order", [(0, ["handed over"]), (4, ["stream 4 waited for", "handed over", "default waited for"])])
+def test_memory_is_handed_over_in_the_order_of_its_stream(home, order):
+    import types
+    torch, said = _FakeTorch(), []
+    torch.now = home
+    torch.current_stream = lambda _: types.SimpleNamespace(synchronize=lambda: said.append("stream %d waited for" % torch.now))
+    torch.default_stream = lambda _: types.SimpleNamespace(synchronize=lambda: said.append("default waited for"))
+    r = B.LinearRunner.__new__(B.LinearRunner)
+    r.torch, r.device, r._raw_stream = torch, None, lambda: torch.now
+    r._allocate_workspace(4096, lambda *a: said.append("handed over"))
+    assert said == order
