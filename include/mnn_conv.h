@@ -400,7 +400,7 @@ MNN_API void mnn_net_destroy(mnn_net_t net);
  * fp32 operands as two halves (hi*hi + lo*hi + hi*lo): TF32 halves, about 21 bits of each value, or, on PAIRS, FP16 halves of rows
  * scaled by a power of two, 24 bits of values down to 2^-16 of their row's largest and 2^-39 of the largest below that.  Relative L2
  * error of fp32 results on normal data: below 1e-6.  An infinity or NaN in x or w gives what the definition gives (slowly in fp32,
- * where such sums are taken a second time).  Pointers need the alignment of their element only; x and w on 16-byte boundaries with
+ * where such sums are taken a second time: up to some 25 us per element of K for a block of 256 x 256 infinite results).  Pointers need the alignment of their element only; x and w on 16-byte boundaries with
  * row strides of a multiple of 16 bytes are read directly, others shifted on the way.  y may be the residual itself (same pointer and stride) and must not
  * overlap x, w or bias.  Nothing is prepared ahead or kept from one run for the next.
  * Rules on pointers, streams and errors as for the convolutions; the current device must be the device of `stream`.

@@ -72,7 +72,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     __shared__ __align__(8) uint64_t tfull_bar[2];
     __shared__ __align__(8) uint64_t tempty_bar[2];
     __shared__ uint32_t tmem_slot;
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, alive;                                 // alive: counted up while sums are taken again
 
     const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -82,6 +82,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     // 128 bytes a clock (64 rows of x: 56 KB read by the tensor core and 72 KB by copies and conversion, per block of K).
     const uint32_t raw_bytes = (a_bytes + b_bytes) * KB, stage_bytes = raw_bytes * (F32 ? 2 : 1), off_b = a_bytes * KB;
     volatile int* abortp = &abort_flag;
+    const volatile int* const alivep = F32 ? &alive : nullptr;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -93,7 +94,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             ptx::mbar_init(ptx::smem_u32(&tfull_bar[s]), 1);
             ptx::mbar_init(ptx::smem_u32(&tempty_bar[s]), kEpiWarps);
         }
-        abort_flag = 0;
+        abort_flag = alive = 0;
         ptx::fence_barrier_init();
         if (!COPY) {
             ptx::prefetch_tensormap(&map_x);
@@ -129,7 +130,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 int fb, mb;
                 linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!ptx::mbar_wait_warp(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp)) {
+                    if (!ptx::mbar_wait_warp(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp, alivep)) {
                         if (lane == 0) failed(kErrProducer);
                         ok = false;
                         break;
@@ -161,7 +162,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         const uint32_t a_lo0 = ((smem_base & 0x3FFFFu) >> 4) | (1u << 16);
         for (long long item = first_item; item < p.items && ok; item += item_step) {
             for (int seg = kb0; seg < kb1 && ok; seg += F32 ? kSegment : kb1 - kb0) {
-                if (!ptx::mbar_wait_warp(ptx::smem_u32(&tempty_bar[acc]), acc_phase ^ 1u, abortp)) {
+                if (!ptx::mbar_wait_warp(ptx::smem_u32(&tempty_bar[acc]), acc_phase ^ 1u, abortp, alivep)) {
                     if (lane == 0) failed(kErrMmaTmem);
                     ok = false;
                     break;
@@ -171,7 +172,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 const int seg_end = F32 ? min(seg + kSegment, kb1) : kb1;
                 uint32_t accumulate = 0;
                 for (int kb = seg; kb < seg_end; ++kb) {
-                    if (!ptx::mbar_wait_warp(ptx::smem_u32(F32 && !COPY ? &low_bar[stage] : &full_bar[stage]), phase, abortp)) {
+                    if (!ptx::mbar_wait_warp(ptx::smem_u32(F32 && !COPY ? &low_bar[stage] : &full_bar[stage]), phase, abortp, alivep)) {
                         if (lane == 0) failed(kErrMmaFull);
                         ok = false;
                         break;
@@ -211,7 +212,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         bool ok = true;
         auto wait_acc = [&]() {
             int got = 1;
-            if (lane == 0) got = ptx::mbar_wait_relaxed(ptx::smem_u32(&tfull_bar[acc]), acc_phase, abortp) ? 1 : 0;
+            if (lane == 0) got = ptx::mbar_wait_relaxed(ptx::smem_u32(&tfull_bar[acc]), acc_phase, abortp, alivep) ? 1 : 0;
             got = __shfl_sync(0xffffffffu, got, 0);
             if (!got && lane == 0) failed(kErrEpilogue);
             ptx::tc_fence_after();
@@ -241,7 +242,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
                 const long long m0 = m_item + ch * 16;
                 const int rows = (int)min(16ll, p.M - m0);
-                if (F32 && n_ok) retake_sums<16>(s, rows, m0, n, static_cast<const float*>(p.x), p.ldx, static_cast<const float*>(p.w), p.ldw, p.K);
+                if (F32 && n_ok) retake_sums<1>(s, rows, m0, n, static_cast<const float*>(p.x), p.ldx, static_cast<const float*>(p.w), p.ldw, p.K, &alive);
                 out.store(p.epi, s, bias, m0, rows, n, n_ok);
             };
             if (F32) {
@@ -317,7 +318,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
             for (int kb = kb0; kb < kb1; ++kb) {
                 int got = 1;
-                if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp) ? 1 : 0;
+                if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp, alivep) ? 1 : 0;
                 got = __shfl_sync(0xffffffffu, got, 0);
                 if (!got) {
                     if (lane == 0) failed(kErrAux);
@@ -360,7 +361,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (turn == group) {
                     int got = 1;
-                    if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&full_bar[stage]), phase, abortp) ? 1 : 0;
+                    if (lane == 0) got = ptx::mbar_wait_bounded(ptx::smem_u32(&full_bar[stage]), phase, abortp, alivep) ? 1 : 0;
                     got = __shfl_sync(0xffffffffu, got, 0);
                     if (!got) {
                         if (lane == 0) failed(kErrAux);
@@ -400,7 +401,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     LinearStore<TYPE, 1> out;
                     out.fetch(p.epi, m, 1, n, true);
                     float s[1] = {sum};
-                    if (F32) retake_sums<1>(s, 1, m, n, static_cast<const float*>(p.x), p.ldx, static_cast<const float*>(p.w), p.ldw, p.K);
+                    if (F32) retake_sums<1>(s, 1, m, n, static_cast<const float*>(p.x), p.ldx, static_cast<const float*>(p.w), p.ldw, p.K, &alive);
                     out.store(p.epi, s, bias, m, 1, n, true);
                 });
         }

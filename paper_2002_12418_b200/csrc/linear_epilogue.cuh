@@ -4,7 +4,9 @@
 #include <cuda_fp16.h>
 
 #include "../../include/mnn_conv.h"
+#include "cluster.cuh"
 #include "linear.h"
+#include "umma.cuh"
 
 namespace mnnb {
 
@@ -92,19 +94,30 @@ struct LinearStore {
 
 // fp32: sums without a finite value are taken again, term by term (an infinity's low half is no number).  The loop is kept out of
 // line and behind one branch: inlined, the compiler ran all of it under predicates for every sum (28 us of 54 at K = 1024).
-static __device__ __noinline__ float retake_sum(const float* x, const float* w, int K)
+// A thread may do this for 64 sums while other roles wait for its accumulator, longer than their waits last (256 x 256 sums on a pair:
+// some 26 us per term): it counts `alive` up, in each of the CTAS whose roles wait, every kRetakeTick terms.  (By whole warps, 32 terms of
+// one sum at a time, it took a quarter of that, but the call then cost sums without an infinity more registers: 3136 x 1024 x 1024 39 -> 42 us.)
+constexpr int kRetakeTick = 8192;
+template <int CTAS>
+static __device__ __noinline__ float retake_sum(const float* x, const float* w, int K, int* alive)
 {
     float t = 0.0f;
     int k = 0;
     for (; k + 8 <= K && t == t; k += 8) {           // (a NaN stays one)
+        if ((k & (kRetakeTick - 1)) == 0) {
+            if (CTAS == 1) atomicAdd(alive, 1);
+            else
+                for (uint32_t r = 0; r < CTAS; ++r)
+                    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], 1;" ::"r"(ptx::map_to_rank(ptx::smem_u32(alive), r)) : "memory");
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) t = fmaf(x[k + j], w[k + j], t);
     }
     for (; k < K && t == t; ++k) t = fmaf(x[k], w[k], t);
     return t;
 }
-template <int NUM>
-__device__ __forceinline__ void retake_sums(float (&s)[NUM], int rows, long long m0, int n, const float* x, long long ldx, const float* w, long long ldw, int K)
+template <int CTAS, int NUM>
+__device__ __forceinline__ void retake_sums(float (&s)[NUM], int rows, long long m0, int n, const float* x, long long ldx, const float* w, long long ldw, int K, int* alive)
 {
     bool any = false;
 #pragma unroll
@@ -112,7 +125,7 @@ __device__ __forceinline__ void retake_sums(float (&s)[NUM], int rows, long long
     if (!any) return;
 #pragma unroll
     for (int j = 0; j < NUM; ++j)
-        if (j < rows && !isfinite(s[j])) s[j] = retake_sum(x + (m0 + j) * ldx, w + (long long)n * ldw, K);
+        if (j < rows && !isfinite(s[j])) s[j] = retake_sum<CTAS>(x + (m0 + j) * ldx, w + (long long)n * ldw, K, alive);
 }
 
 template <int TYPE>

@@ -89,7 +89,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     __shared__ __align__(8) uint64_t tfull_bar[2];
     __shared__ __align__(8) uint64_t tempty_bar[2];
     __shared__ uint32_t tmem_slot;
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, alive;         // alive: counted up while sums are taken again, by both CTAs
 
     const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank();
@@ -98,6 +98,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     // stage: [A][B], for fp32 followed by [A low][B low]
     const uint32_t raw_bytes = kTileBytes + (uint32_t)(p.bm >> 1) * 128, stage_bytes = raw_bytes * (F32 ? 2 : 1);
     volatile int* abortp = &abort_flag;
+    const volatile int* const alivep = F32 ? &alive : nullptr;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -108,7 +109,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             ptx::mbar_init(ptx::smem_u32(&tfull_bar[s]), 1);
             ptx::mbar_init(ptx::smem_u32(&tempty_bar[s]), 2 * kEpiWarps<TYPE>);
         }
-        abort_flag = 0;
+        abort_flag = alive = 0;
         ptx::fence_barrier_init();
         ptx::prefetch_tensormap(&map_x);
         ptx::prefetch_tensormap(&map_w);
@@ -137,7 +138,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             linear_item(item, p.n_fblocks, p.n_mblocks, &fb, &mb);
             const int w_row = (fb * 2 + (int)rank) * kRows, x_row = mb * p.bm + (int)rank * (p.bm >> 1);
             for (int kb = 0; kb < p.k_blocks; ++kb) {
-                if (!ptx::mbar_wait_warp(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp)) {
+                if (!ptx::mbar_wait_warp(ptx::smem_u32(&empty_bar[stage]), phase ^ 1u, abortp, alivep)) {
                     if (lane == 0) failed(kErrProducer);
                     ok = false;
                     break;
@@ -169,7 +170,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             bool ok = true;
             for (long long item = pair; item < p.items && ok; item += n_pairs)
                 for (int seg = 0; seg < p.k_blocks && ok; seg += F32 ? kSegment : p.k_blocks) {
-                    if (!ptx::mbar_wait_warp(ptx::smem_u32(&tempty_bar[acc]), acc_phase ^ 1u, abortp)) {
+                    if (!ptx::mbar_wait_warp(ptx::smem_u32(&tempty_bar[acc]), acc_phase ^ 1u, abortp, alivep)) {
                         if (lane == 0) failed(kErrMmaTmem);
                         ok = false;
                         break;
@@ -178,7 +179,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     const uint32_t d_tmem = tmem_base + acc * (uint32_t)kPairN;
                     const int seg_end = F32 ? min(seg + kSegment, p.k_blocks) : p.k_blocks;
                     for (int kb = seg; kb < seg_end; ++kb) {
-                        if (!ptx::mbar_wait_warp(ptx::smem_u32(&full_bar[stage]), phase, abortp)) {
+                        if (!ptx::mbar_wait_warp(ptx::smem_u32(&full_bar[stage]), phase, abortp, alivep)) {
                             if (lane == 0) failed(kErrMmaFull);
                             ok = false;
                             break;
@@ -217,7 +218,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         uint32_t acc = 0, acc_phase = 0;
         auto wait_acc = [&]() {
             int got = 1;
-            if (lane == 0) got = ptx::mbar_wait_relaxed(ptx::smem_u32(&tfull_bar[acc]), acc_phase, abortp) ? 1 : 0;
+            if (lane == 0) got = ptx::mbar_wait_relaxed(ptx::smem_u32(&tfull_bar[acc]), acc_phase, abortp, alivep) ? 1 : 0;
             got = __shfl_sync(0xffffffffu, got, 0);
             if (!got && lane == 0) failed(kErrEpilogue);
             ptx::tc_fence_after();
@@ -288,7 +289,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                             const int down = -(w_up + __shfl_sync(0xffffffffu, ups, j)), half = down >> 1;
                             sum[c][j] = sum[c][j] * power_of_two(half) * power_of_two(down - half);
                         }
-                        if (n_ok) retake_sums<16>(sum[c], rows, m0, n, p.x, p.ldx, p.w, p.ldw, p.K);
+                        if (n_ok) retake_sums<2>(sum[c], rows, m0, n, p.x, p.ldx, p.w, p.ldw, p.K, &alive);
                         // (eight rows of the residual at a time, and after the call: more of them beside the sums went to local
                         // memory.  3136 x 1024 x 1024 with a residual 45 -> 39 us, without one 45 -> 33)
                         LinearStore<TYPE, 8> part;

@@ -71,7 +71,8 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
 
 // A wait spins kFastPolls times, then polls with ~100 ns sleeps until kWaitLimitNs of wall time (the GPU's
 // global timer) have passed since it began sleeping: about one second, after which it returns false.
-// `abort_flag` (shared memory) lets one role's failure end the others' waits early.
+// `abort_flag` (shared memory) lets one role's failure end the others' waits early.  `alive` (shared memory, or null), where given, is
+// counted up by a role that does long work of its own: the time runs from its last change.
 constexpr uint32_t kFastPolls = 1u << 14;
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;
 
@@ -82,14 +83,29 @@ __device__ __forceinline__ unsigned long long global_timer_ns()
     return t;
 }
 
-__device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+struct WaitClock {
+    unsigned long long t0;
+    const volatile int* alive;
+    int seen;
+    __device__ __forceinline__ explicit WaitClock(const volatile int* a) : t0(global_timer_ns()), alive(a), seen(a ? *a : 0) {}
+    __device__ __forceinline__ bool out()
+    {
+        if (alive && *alive != seen) {
+            seen = *alive;
+            t0 = global_timer_ns();
+        }
+        return global_timer_ns() - t0 > kWaitLimitNs;
+    }
+};
+
+__device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort_flag, const volatile int* alive = nullptr)
 {
     for (uint32_t i = 0; i < kFastPolls; ++i)
         if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_timer_ns();
+    WaitClock clock(alive);
     for (uint32_t i = 0;; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 63u) == 0 && (*abort_flag || global_timer_ns() - t0 > kWaitLimitNs)) return false;
+        if ((i & 63u) == 0 && (*abort_flag || clock.out())) return false;
         __nanosleep(100);
     }
 }
@@ -97,28 +113,28 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
 // The same for a whole converged warp: every poll is voted on, so that all lanes leave together and with one answer (lanes
 // that disagreed would wait for each other for good at the next warp-wide instruction), and the code behind the wait stays
 // uniform to the compiler.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, const volatile int* alive = nullptr)
 {
     for (uint32_t i = 0; i < kFastPolls; ++i)
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    const unsigned long long t0 = global_timer_ns();
+    WaitClock clock(alive);
     for (uint32_t i = 0;; ++i) {
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-        if ((i & 63u) == 0 && __any_sync(0xffffffffu, *abort_flag || global_timer_ns() - t0 > kWaitLimitNs)) return false;
+        if ((i & 63u) == 0 && __any_sync(0xffffffffu, *abort_flag || clock.out())) return false;
         __nanosleep(100);
     }
 }
 
 // The same bound for warps that can afford to wait: sleeps between polls from the start, so that
 // waiting warps do not take issue slots from the warps they are waiting for.
-__device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+__device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity, volatile int* abort_flag, const volatile int* alive = nullptr)
 {
     if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_timer_ns();
+    WaitClock clock(alive);
     for (uint32_t i = 0;; ++i) {
         __nanosleep(64);
         if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 63u) == 0 && (*abort_flag || global_timer_ns() - t0 > kWaitLimitNs)) return false;
+        if ((i & 63u) == 0 && (*abort_flag || clock.out())) return false;
     }
 }
 

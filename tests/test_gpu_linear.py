@@ -316,3 +316,34 @@ def test_refusals_of_tensors():
     both = torch.zeros(4, 24, dtype=torch.bfloat16, device="cuda")
     B.LinearRunner(4, 8, 16, "bf16", ldx=24, ldy=24).run(both[:, :16], w, y=both[:, 16:])
     torch.cuda.synchronize()
+
+
+# every sum infinite and K so long that taking the sums of one work item again lasts longer than a wait may (1.8 and 1.5 s, a wait one
+# second): a second item's waits must not run out meanwhile.  A record of two SMs gives one SM, or the pair of them, two items at small
+# sizes.
+@pytest.mark.parametrize("M,N,K,form", [(96, 384, 1 << 18, B.LINEAR_TILES), (256, 512, 1 << 16, B.LINEAR_PAIRS)])
+def test_infinite_sums_of_a_very_long_k(M, N, K, form):
+    import torch
+    before = B.mnn_get_calibration()
+    try:
+        record = list(before)
+        record[7] = 2
+        B.mnn_set_calibration(record)
+        r = B.LinearRunner(M, N, K)
+    finally:
+        B.mnn_set_calibration(before)
+    assert r.info.form == form and r.info.split == 1 and r.info.items > (2 if form == B.LINEAR_TILES else 1)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    x, w = torch.full((M, K), 0.5, device="cuda"), torch.ones(N, K, device="cuda")
+    at = torch.randint(0, K, (M,), generator=g, device="cuda")
+    rows = torch.arange(M, device="cuda")
+    x[rows, at] = torch.where(rows % 2 == 0, float("inf"), float("-inf"))
+    y = r.run(x, w)
+    torch.cuda.synchronize()
+    assert r.device_status() == 0
+    assert (y[0::2] == float("inf")).all() and (y[1::2] == float("-inf")).all()
+    x[rows, at] = 0.5                                # and the workspace is good for the next run
+    y = r.run(x, w)
+    torch.cuda.synchronize()
+    assert r.device_status() == 0 and (y == 0.5 * K).all()
