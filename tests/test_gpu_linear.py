@@ -347,3 +347,46 @@ def test_infinite_sums_of_a_very_long_k(M, N, K, form):
     y = r.run(x, w)
     torch.cuda.synchronize()
     assert r.device_status() == 0 and (y == 0.5 * K).all()
+
+
+# GELU's tail: with sums that are exact (one term, of 8 bits), what is left is the evaluation of v h(|v|) or v (1 - h), h = erfc(|v| / sqrt 2) / 2 =
+# e^(-v^2/2) q(t), t = 1 / (1 + c |v|).  Relative errors in units of 2^-24: the exponent v^2 / 2 is rounded twice and its factor once, 1.5 v^2;
+# the exponential 4; t 3 (fp32: 2.2) that q's slope of 2.7 makes 8 (6); q's own roundings 6.5; its fit 32 (0.5); three products and a difference 3.
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("M,N,form", [(1, 4096, B.LINEAR_FEW), (64, 4096, B.LINEAR_TILES), (2048, 4096, B.LINEAR_PAIRS)])
+def test_gelu_far_from_zero(M, N, form, dtype):
+    import math
+
+    import torch
+    K = 256
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    v = (torch.arange(N, device="cuda") / (N / 24.0) - 12.0).bfloat16()          # -12 to 12 in 8 bits
+    x, w = torch.zeros(M, K, dtype=t, device="cuda"), torch.zeros(N, K, dtype=t, device="cuda")
+    x[:, 3], w[:, 3] = 1.0, v.to(t)
+    r = B.LinearRunner(M, N, K, dtype, act="gelu")
+    assert r.info.form == form
+    got = host(r.run(x, w))
+    s = host(v)
+    want = np.array([0.5 * a * math.erfc(-a / math.sqrt(2.0)) for a in s])
+    err = (1.5 * s * s + (20.0 if dtype == "fp32" else 54.0)) * 2.0 ** -24 * np.abs(want)
+    err += HALF_EPS[dtype] * (np.abs(want) + err) + (2.0 ** -25 if dtype == "fp16" else 0.0)
+    over = np.abs(got - want[None, :]) - err[None, :]
+    assert (over <= 0).all(), (over.max(), s[over.max(0).argmax()])
+
+
+def test_gelu_of_infinities_and_far_values():
+    import torch
+    inf = float("inf")
+    for dtype, N in (("fp32", 8), ("bf16", 8), ("fp32", 300000), ("bf16", 300000)):
+        t = torch.float32 if dtype == "fp32" else torch.bfloat16
+        w = torch.zeros(N, 8, dtype=t, device="cuda")
+        w[:8, 0] = torch.tensor([inf, -inf, float("nan"), 1e38, -1e38, -40.0, 1e19, -1e19], device="cuda").to(t)
+        x = torch.zeros(1, 8, dtype=t, device="cuda")
+        x[0, 0] = 1.0
+        r = B.LinearRunner(1 if N == 8 else 40, N, 8, dtype, act="gelu")
+        y = r.run(x if N == 8 else x.repeat(40, 1), w).float()
+        v = w[:8, 0].float()
+        for row in (y[0], y[-1]):
+            assert row[0] == inf and torch.isnan(row[1:3]).all()                 # minus infinity times nothing
+            # fp32 operands on tiles are two halves of 11 bits, each off by less than 2^-10 of it: 2^-20 of a value (the sum is 1 * v)
+            assert ((row[[3, 6]] - v[[3, 6]]).abs() <= 2.0 ** -20 * v[[3, 6]]).all() and (row[[4, 5, 7]] == 0).all() and (row[8:] == 0).all()
