@@ -397,7 +397,8 @@ MNN_API void mnn_net_destroy(mnn_net_t net);
  * x [M][ldx], w [N][ldw], bias [N] (NULL = zeros), residual [M][ldr] and y [M][ldy] are of ONE type (opts.type); within a row the
  * elements are contiguous, rows may be any number of elements apart that is not smaller than their length.  Sums, bias,
  * activation and residual are evaluated in fp32 and rounded once, at the store.  16-bit operands enter the tensor core as they are,
- * fp32 operands as two halves (hi*hi + lo*hi + hi*lo): TF32 halves, about 21 bits of each value, or, on PAIRS, FP16 halves of rows
+ * fp32 operands as two halves (hi*hi + lo*hi + hi*lo): TF32 halves, about 22 bits of each value (2^-22 of it at most
+ * is rounded off; the product of two low halves, 2^-22 of a product on average, is left out), or, on PAIRS, FP16 halves of rows
  * scaled by a power of two, 24 bits of values down to 2^-16 of their row's largest and 2^-39 of the largest below that.  Relative L2
  * error of fp32 results on normal data: below 1e-6.  An infinity or NaN in x or w gives what the definition gives (slowly in fp32,
  * where such sums are taken a second time: up to some 25 us per element of K for a block of 256 x 256 infinite results).  Pointers need the alignment of their element only; x and w on 16-byte boundaries with

@@ -10,8 +10,10 @@
 // distributed shared memory (cluster.cuh): deterministic, one launch, no workspace.
 //
 // 16-bit operands go to the tensor core as they are.  fp32 operands are cut in two: the tensor core reads the high 19 bits
-// (TF32, dropping the low 13), and `converter` warps write lo = v - trunc(v), exact in fp32, beside each tile; hi*hi goes to one
-// accumulator, lo*hi + hi*lo to another (the dropped lo*lo is 2^-22 of a product).  The tensor core's own additions cut their
+// (TF32, dropping the low 13), and `converter` warps write lo = v - trunc(v) beside each tile, with half a unit added so that dropping ITS low bits
+// rounds it; hi*hi goes to one accumulator, lo*hi + hi*lo to another.  What is lost of a product: 2^-22 at most by the rounding of either low half, and lo*lo,
+// 2^-22 on average (2^-20 at most).  relL2 with N(0, 1) data 3.5e-7 at K = 96 and 4.2e-7 at 2048 to 8192 (low halves cut off: 5.6e-7 and 6.3e-7, and 4 % faster: 128 x
+// 1024 x 32000 77 -> 80 us; fp32 products by a library 1.8e-7 at K = 96 and 7e-7 to 1.1e-6).  The tensor core's own additions cut their
 // result off instead of rounding it, which over a long K loop grows to a bias of about 2^-25 per step; so after every kSegment
 // blocks of K both accumulators are added to fp32 registers, which round.  Sums that this leaves without a finite value
 // (an infinity's low half is no number) are taken again by their thread, term by term in fp32.
@@ -478,12 +480,12 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
         // (linear_few.cu); two features a warp, and one, and several warps per K loop, where that leaves fewer than 16 warps per SM.
         // The more rows, the sooner the sums cost more than the stream.  Here and on tiles, us: BF16 1 x 2048 x 8192 6.2 and 8.2, 1 x 4096 x
         // 16384 28.1 and 24.5, 1 x 1008 x 131072 61 and 44, 2 x 1024 x 8192 5.6 and 6.8, 2 x 4096 x 4096 11.7 and 8.3, 4 x 1024 x 1000 3.5 and
-        // 5.1, 4 x 4096 x 4096 12.3 and 8.4; fp32, whose halves cost tiles more, 2 x 2048 x 65536 88 and 131, 4 x 1024 x 8192 8.7 and 14.4,
-        // 4 x 8192 x 8192 81 and 70; rows that tiles have to lay out first: BF16 1 x 1001 x 131072 92 and 155, 2 x 4099 x 16384 53 and 73,
-        // 4 x 1022 x 4314 11.0 and 14.3, 4 x 4097 x 4096 26 and 23, fp32 4 x 1023 x 20000 51 and 69.  Groups: fp32 100 x 256 x 48 2.9 and 6.8,
-        // 8 x 1024 x 1000 6.8 and 7.9, 12 x 1024 x 1000 8.8 and 8.0, and 16 x 12009 x 94, which tiles have to lay out first, 20.4 and
-        // 31.9; BF16 100 x 256 x 48 2.5 and 3.5, 6 x 512 x 512 2.9 and 5.1, 8 x 704 x 1472 6.7 and 5.3; and with many warps
-        // 1000 x 64 x 64 7.8 and 3.3 (fp32 6.2 and 5.1).
+        // 5.1, 4 x 4096 x 4096 12.3 and 8.4; fp32, whose halves cost tiles more, 2 x 2048 x 65536 88 and 136, 4 x 1024 x 8192 13.8 and 16.3,
+        // 4 x 8192 x 8192 82 and 75; rows that tiles have to lay out first: BF16 1 x 1001 x 131072 92 and 155, 2 x 4099 x 16384 53 and 73,
+        // 4 x 1022 x 4314 11.0 and 14.3, 4 x 4097 x 4096 26 and 23, fp32 4 x 1023 x 20000 50 and 72.  Groups: fp32 100 x 256 x 48 2.8 and 7.2,
+        // 8 x 1024 x 1000 6.8 and 7.9, 12 x 1024 x 1000 8.8 and 8.0, and 16 x 12009 x 94, which tiles have to lay out first, 20.5 and
+        // 34.6; BF16 100 x 256 x 48 2.5 and 3.5, 6 x 512 x 512 2.9 and 5.1, 8 x 704 x 1472 6.7 and 5.3; and with many warps
+        // 1000 x 64 x 64 7.8 and 3.3 (fp32 5.8 and 5.4).
         t.form = MNN_LINEAR_FEW;
         t.bm = s.M < 4 ? s.M : 4;
         t.feats = s.M > 2 || s.N / 2 >= 16ll * num_sms ? 2 : 1;
@@ -527,9 +529,9 @@ LinearTiling linear_tiling(const LinearShape& s, bool unaligned, int num_sms)
     }
     // Pairs of SMs (linear_pair.cu): half the rows of x per CTA, so that the tensor core and not the delivery decides.  fp32 (as
     // two FP16 halves, three products) needs a pass over both operands first, as rows that are not aligned do.  Here and on tiles, fp32:
-    // 1024 x 4096 x 1024 66 and 79 us, 1024 x 1024 x 1024 24 and 28, 384 x 2048 x 2048 39 and 43, 512 x 4096 x 1024 (32 items of four
-    // CTAs) 63 and 40; a short K does not earn the pass: 12544 x 128 x 256 19.7 and 13.9.
-    // Fewer rows only where tiles have to lay fp32 operands out as well: 80 x 1001 x 8000 39 and 45, but 128 x 1024 x 32000 98 and 76.
+    // 1024 x 4096 x 1024 65 and 84 us, 1024 x 1024 x 1024 24 and 30, 384 x 2048 x 2048 39 and 50, 512 x 4096 x 1024 (32 items of four
+    // CTAs) 61 and 46; a short K does not earn the pass: 12544 x 128 x 256 20.0 and 14.2.
+    // Fewer rows only where tiles have to lay fp32 operands out as well: 80 x 1001 x 8000 37 and 45, but 128 x 1024 x 32000 98 and 80.
     const long long pairs = num_sms / 2;
     if (s.M < (f32 && strides ? 72 : 192) || t.form == MNN_LINEAR_COPIED || (f32 && s.K < 192) || pairs < 1) return t;
     const long long blocks = ((long long)s.K + 63) / 64, ld = blocks * 64;

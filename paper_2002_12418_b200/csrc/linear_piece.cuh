@@ -5,8 +5,13 @@
 
 namespace mnnb {
 
-// lo = v - trunc(v) (no number for an infinity, which makes its sums none either: they are taken again)
-__device__ __forceinline__ float low_half(float v) { return v - __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
+// lo = v - trunc(v), exact, and half a unit of the 11 bits that the tensor core reads of it, which so rounds what it cuts off.  (What has no
+// finite value may have any low half: its high one is not finite either, and its sums are taken again.)
+__device__ __forceinline__ float low_half(float v)
+{
+    const float lo = v - __uint_as_float(__float_as_uint(v) & 0xffffe000u);
+    return __uint_as_float(__float_as_uint(lo) + 0x1000u);
+}
 __device__ __forceinline__ float4 low_half(float4 v) { return make_float4(low_half(v.x), low_half(v.y), low_half(v.z), low_half(v.w)); }
 
 // 16 bytes that start `by` bytes into the 32 of p and q; by < 16, a multiple of EB.

@@ -390,3 +390,25 @@ def test_gelu_of_infinities_and_far_values():
             assert row[0] == inf and torch.isnan(row[1:3]).all()                 # minus infinity times nothing
             # fp32 operands on tiles are two halves of 11 bits, each off by less than 2^-10 of it: 2^-20 of a value (the sum is 1 * v)
             assert ((row[[3, 6]] - v[[3, 6]]).abs() <= 2.0 ** -20 * v[[3, 6]]).all() and (row[[4, 5, 7]] == 0).all() and (row[8:] == 0).all()
+
+
+# fp32 on tiles, one term: hi hi + lo hi + hi lo with hi the upper 11 bits of a value and lo what is left of it, rounded to 11 bits.  lo is smaller
+# than 2^-10 of the value (of its power of two), so that its rounding is off by at most half of 2^-10 2^-11: 2^-22.  Beside the missing lo lo, which is
+# known, the product is off by 2^-22 for each operand, by 2^-24 for the rounding of the sum, and by what is cut off lo hi + hi lo, 2^-23 of it, 2^-32.
+@pytest.mark.parametrize("offset", [0, 1])
+def test_low_halves_are_rounded(offset):
+    import torch
+    M, N, K = 64, 4096, 256
+    x, w = make(torch, 1, (M, K), K, "fp32", offset=offset), make(torch, 2, (N, K), K, "fp32", offset=offset)
+    x[:, :7], x[:, 8:] = 0.0, 0.0
+    w[:, 7].copy_(w[:, 3])
+    r = B.LinearRunner(M, N, K)
+    assert r.info.form == B.LINEAR_TILES                      # (COPIED where the tensors start off 16 bytes)
+    got = host(r.run(x, w))
+    assert r.device_status() == 0
+    a, b = x[:, 7].contiguous(), w[:, 7].contiguous()
+    lo = lambda t: host(t) - host((t.view(torch.int32) & -8192).view(torch.float32))  # noqa: E731
+    product = host(a)[:, None] * host(b)[None, :]
+    want = product - lo(a)[:, None] * lo(b)[None, :]
+    over = np.abs(got - want) - (2 * 2.0 ** -22 + 2.0 ** -24 + 2.0 ** -32) * np.abs(product)
+    assert (over <= 0).all(), over.max()
