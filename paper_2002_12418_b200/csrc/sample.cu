@@ -990,7 +990,7 @@ sample_kernel(SampleParams p)
     }
 }
 
-// ---- BF16 rows: by values (long ones of which top-k or top-p may cut something)
+// ---- BF16 rows: by values (long ones of which top-p, or very long ones of which top-k, may cut something)
 //
 // BF16 logits have few values: below a largest logit of 10, 1568 down to 2^-9.  A bin per value makes counts enough: its mass is
 // the count times one weight, so weights are evaluated once per value and not once per element (the row's passes were bound by
@@ -1001,6 +1001,7 @@ sample_kernel(SampleParams p)
 // is found by halving the range of keys.
 constexpr int kValues = 4096;
 constexpr int kNearZero = 0x3b00;        // the bits of 2^-9
+constexpr int kLongByCount = 32768;      // logits of a row from which on top-k alone goes by values (launch_sample)
 
 struct SharedValues {
     RowGiven row;
@@ -1658,11 +1659,14 @@ cudaError_t launch_sample(const SampleShape& s, const SampleTiling& t, const Sam
     p.a = a;
     switch (s.type) {
         case MNN_TYPE_FP32: return run_sample<MNN_TYPE_FP32>(s, t, p, stream);
-        // By values where a border is looked for, in rows of more logits than there are bins.  us, by values and not, top-p 0.9: 512 x 1000
-        // 76.6 and 28.0, 1 x 4000 16.4 and 18.0, 512 x 8000 52.5 and 57.0, 512 x 32000 97 and 124; top-k 300 x 131072 122 and 142 (but 512 x
-        // 32000 81 and 65); neither: 1 x 131072 16.7 and 12.3, 512 x 32000 73 and 49.
+        // By values where top-p is given and rows have more logits than there are bins; with top-k alone, whose counts cost either kernel the
+        // same, where rows are long.  us, by values and not.  Top-p 0.9: 512 x 1000 76.6 and 28.0, 1 x 5000 18.0 and 19.8, 512 x 8000 52 and 57, 512 x
+        // 32000 96 and 141, 512 x 131072 242 and 484 (with top-k 50 as well 512 x 8000 53 and 39, 512 x 32000 87 and 84, 512 x 131072 211 and 244; what
+        // the arrays hold is not known here).  Top-k 50 alone: 512 x 5000 48 and 32, 512 x 16000 58 and 44, 512 x 32000 81 and 78, 1 x 32000 13.6 and
+        // 13.9, 512 x 64000 134 and 150, 512 x 131072 198 and 231; top-k 1000 512 x 16000 63 and 51, 512 x 32000 94 and 93, 512 x 64000 156 and 191.
+        // Neither, or arrays that cut nothing: 1 x 131072 17.1 and 12.5, 512 x 32000 74 and 53.
         case MNN_TYPE_BF16:
-            return s.vocab > kValues && (a.top_k || a.top_p) ? run_values(s, t, p, stream) : run_sample<MNN_TYPE_BF16>(s, t, p, stream);
+            return (a.top_p && s.vocab > kValues) || (a.top_k && s.vocab > kLongByCount) ? run_values(s, t, p, stream) : run_sample<MNN_TYPE_BF16>(s, t, p, stream);
         default: return run_sample<MNN_TYPE_FP16>(s, t, p, stream);
     }
 }
