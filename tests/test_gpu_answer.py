@@ -88,3 +88,44 @@ def test_block_of_tokens_and_vocabulary():
         for i in range(M):
             t, q, _ = oracle.sample_row(f(logits[i]), float(u[i]), top_p=float(p[i].double()))
             assert int(token[i]) == t and abs(float(prob[i]) - q) <= 2.0 ** -23 * q
+
+
+# product, product and draw again and again on one stream over the same buffers, with inputs whose size changes by 2^3 from one to the next: each
+# kernel may start while the one before it still runs, and has to see what that one writes
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,D,F,V", [(1, 256, 512, 1000), (4, 512, 512, 3000), (33, 129, 257, 1001), (300, 512, 1024, 4100), (1500, 640, 1300, 1040)])
+def test_chains_over_the_same_buffers(M, D, F, V, dtype):
+    import torch
+    t = torch.float32 if dtype == "fp32" else torch.bfloat16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M)
+    xs = [(torch.randn(M, D, generator=g, device="cuda") * 2.0 ** (i % 7 * 3 - 9)).to(t) for i in range(60)]
+    w1, w2 = [(torch.randn(n, k, generator=g, device="cuda") * k ** -0.5).to(t) for n, k in ((F, D), (V, F))]
+    a, b, draw = B.LinearRunner(M, F, D, dtype, act="relu"), B.LinearRunner(M, V, F, dtype), B.SampleRunner(M, V, dtype)
+    h, logits = torch.empty(M, F, device="cuda", dtype=t), torch.empty(M, V, device="cuda", dtype=t)
+    u, p = torch.rand(M, generator=g, device="cuda"), torch.full((M,), 0.9, device="cuda")
+
+    def buffers():
+        return [(torch.empty(M, dtype=torch.int32, device="cuda"), torch.empty(M, device="cuda")) for _ in xs]
+
+    def go(out, between=lambda: None):
+        for x, (token, prob) in zip(xs, out):
+            a.run(x, w1, y=h)
+            between()
+            b.run(h, w2, y=logits)
+            between()
+            draw.run(logits, u, top_p=p, token=token, prob=prob)
+            between()
+
+    want, eager, replayed = buffers(), buffers(), buffers()
+    go(want, torch.cuda.synchronize)
+    go(eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go(replayed)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for out in (eager, replayed):
+        assert all(torch.equal(c[0], d[0]) and torch.equal(c[1], d[1]) for c, d in zip(want, out))
+    assert a.device_status() == 0 and b.device_status() == 0

@@ -412,3 +412,32 @@ def test_low_halves_are_rounded(offset):
     want = product - lo(a)[:, None] * lo(b)[None, :]
     over = np.abs(got - want) - (2 * 2.0 ** -22 + 2.0 ** -24 + 2.0 ** -32) * np.abs(product)
     assert (over <= 0).all(), over.max()
+
+
+# tensors that start off 16 bytes, fetched by copier warps: several work items to a CTA (a record of three SMs), so that the ring of stages goes on
+# from one to the next at every phase, and K loops shared by a cluster.  The form is the one that info names, or COPIED where that is TILES or PAIRS.
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("sms,M,K,N", [(3, 70, 264, 1300), (3, 130, 1032, 900), (3, 33, 72, 2000), (148, 40, 4104, 500), (148, 12, 4104, 400)])
+def test_copiers_over_many_items_and_shared_loops(sms, M, K, N, dtype):
+    before = B.mnn_get_calibration()
+    try:
+        record = list(before)
+        record[7] = sms
+        B.mnn_set_calibration(record)
+        _, info = run_case(M, K, N, dtype, "relu", "after", pads=(8, 16, 1, 0), offset=1, seed=K)
+    finally:
+        B.mnn_set_calibration(before)
+    assert info.form in (B.LINEAR_TILES, B.LINEAR_PAIRS) and (info.items > sms if sms == 3 else info.split > 1)
+
+
+def test_the_status_word_is_read_and_cleared():
+    import torch
+    r = B.LinearRunner(40, 300, 256)
+    x, w = torch.ones(40, 256, device="cuda"), torch.ones(300, 256, device="cuda")
+    r.run(x, w)
+    assert r.device_status() == 0
+    at = r._ws_ptr - r.workspace.data_ptr()
+    r.workspace[at:at + 4].view(torch.int32).fill_(53)       # as a wait that ran out leaves it
+    r.run(x, w)
+    assert r.device_status() == 53 and r.device_status() == 0
+    assert (r.run(x, w) == 256).all() and r.device_status() == 0

@@ -296,3 +296,22 @@ def test_logits_and_draw_together():
         table = torch.randn(V, K, generator=g, device="cuda").mul_(0.3).to(t)
         logits = B.LinearRunner(M, V, K, dtype).run(h, table)
         check(logits, torch.rand(M, generator=g, device="cuda"), top_p=torch.full((M,), 0.9, device="cuda"))
+
+
+# rows of the distribution further apart than their length; what lies between them is left as it was
+@pytest.mark.parametrize("dtype,vocab", [("fp32", 1001), ("bf16", 40001), ("fp16", 70000)])
+def test_distribution_rows_apart(dtype, vocab):
+    import torch
+    rows, pad = 5, 7
+    l, u, g = make(torch, 21, rows, vocab, dtype)
+    l = l.contiguous()
+    p = torch.rand(rows, generator=g, device="cuda")
+    want = B.SampleRunner(rows, vocab, dtype).run(l, u, top_p=p, probs=True)
+    plan = B.mnn_sample_plan(rows, vocab, B.make_sample_opts(dtype, 0, vocab + pad))
+    token, prob = torch.empty(rows, dtype=torch.int32, device="cuda"), torch.empty(rows, device="cuda")
+    probs = torch.full((rows, vocab + pad), 7.0, device="cuda")
+    B.mnn_sample_run(plan, l.data_ptr(), u.data_ptr(), None, None, p.data_ptr(), None, token.data_ptr(), prob.data_ptr(), probs.data_ptr(),
+                     torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    B.mnn_sample_destroy(plan)
+    assert torch.equal(token, want[0]) and torch.equal(prob, want[1]) and torch.equal(probs[:, :vocab], want[2]) and (probs[:, vocab:] == 7.0).all()
