@@ -465,7 +465,10 @@ MNN_API void mnn_linear_destroy(mnn_linear_plan_t plan);
  *                 their whole mass.  u in [0, 1); what lies outside counts as the nearest number inside, a NaN as 0.
  *   prob          w of the token / mass of what stayed.
  *   probs         the same for every i (0 for those that did not stay).
- * Weights are evaluated in fp64 (to 5e-11 of each) and summed as integers, so that a token does not depend on the order of additions.
+ * Weights are evaluated in fp64 (to 5e-11 of each), rounded to units of 2^-scale_log2 of the row's largest (info; 43 to 45) and summed as
+ * integers, so that a token does not depend on the order of additions.  Sums are off by half a unit per candidate at most: where p of
+ * top_p is nearer to 1 than vocab^2 2^-scale_log2 / 2 (2.4e-4 for 131072), the border may lie some candidates beside the exact one, whose mass together is
+ * below vocab / 2 units; and a min_p below half a unit cuts what weighs less than that.
  *
  * logits [rows][ld] of opts.type, temperature, top_p, min_p, u (float) and top_k (int) are DEVICE arrays of one value per row;
  * each but u may be NULL (temperature 1, nothing cut).  token [rows] int, prob [rows] float or NULL, probs [rows][ld_probs]

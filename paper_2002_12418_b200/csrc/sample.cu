@@ -4,10 +4,12 @@
 // (those before which less than p of the mass of the k lies) and by min-p (w_i >= min_p); the token is the lowest index at which
 // the running mass of what is kept, in index order, exceeds u times the whole.
 //
-// Every decision compares sums of weights with a border, so the sums have to be exact to well below one weight and must not
+// Every decision compares sums of weights with a border, so the sums have to be exact to below one weight and must not
 // depend on the order in which threads add.  A weight is therefore evaluated in fp64 (relative error 5e-11) and held as an
-// integer in units of 2^-scale (scale = 62 - log2 of the vocabulary, at most 45): sums are exact, in any order, and no atomic
-// changes a result.
+// integer in units of 2^-scale (scale = 62 - log2 of the vocabulary, at most 45): the sums are of these integers, in any order, and no
+// atomic changes a result.  The rounding to units makes them off by vocab / 2 units at most (by the root of that where roundings are
+// independent; equals round alike).  A border of top-p lies at weights of at least (1 - p) / vocab, so that is below one weight unless
+// 1 - p < vocab^2 2^-scale / 2.  (110674 values in steps of 0.5, T 0.29, p = 1 - 3.6e-7: one element of 1e-10 more than 11974 stays.)
 //
 // A cluster of CTAs holds a row in shared memory (read once from HBM).  No sort: the border of a prefix is one value of l.
 //   top-k: a histogram of counts over 1024 bins of m - l (16 octaves of 64 bins, so that the bulk of a row spreads over many bins
