@@ -431,7 +431,7 @@ typedef struct {
     int features_per_item;
     int split;                       /* CTAs of a cluster (FEW: warps of a CTA) that share an item's K loop */
     int launches_per_run;            /* 2 where operands are laid out in the workspace first */
-    int reserved;
+    int form_unaligned;              /* MNN_LINEAR_* where x or w starts elsewhere: FEW, the form of laid-out rows (strides), or COPIED */
     long long items;
     long long workspace_bytes;       /* the status word, and the operands laid out anew */
 } mnn_linear_info;

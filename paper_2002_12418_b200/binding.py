@@ -91,7 +91,7 @@ class LinearOpts(ctypes.Structure):
 class LinearInfo(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int), ("N", ctypes.c_int), ("K", ctypes.c_int), ("type", ctypes.c_int), ("act", ctypes.c_int),
                 ("residual", ctypes.c_int), ("form", ctypes.c_int), ("rows_per_item", ctypes.c_int), ("features_per_item", ctypes.c_int),
-                ("split", ctypes.c_int), ("launches_per_run", ctypes.c_int), ("reserved", ctypes.c_int), ("items", ctypes.c_longlong),
+                ("split", ctypes.c_int), ("launches_per_run", ctypes.c_int), ("form_unaligned", ctypes.c_int), ("items", ctypes.c_longlong),
                 ("workspace_bytes", ctypes.c_longlong)]
 
 

@@ -108,6 +108,7 @@ int mnn_linear_plan_query(mnn_linear_plan_t p, mnn_linear_info* info)
     info->M = p->s.M; info->N = p->s.N; info->K = p->s.K;
     info->type = p->s.type; info->act = p->act; info->residual = p->residual;
     info->form = p->tiling.form;
+    info->form_unaligned = p->unaligned.form;
     info->rows_per_item = p->tiling.bm;
     info->features_per_item = p->tiling.feats;
     info->split = p->tiling.split;

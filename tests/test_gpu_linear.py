@@ -403,7 +403,7 @@ def test_low_halves_are_rounded(offset):
     x[:, :7], x[:, 8:] = 0.0, 0.0
     w[:, 7].copy_(w[:, 3])
     r = B.LinearRunner(M, N, K)
-    assert r.info.form == B.LINEAR_TILES                      # (COPIED where the tensors start off 16 bytes)
+    assert r.info.form == B.LINEAR_TILES and r.info.form_unaligned == B.LINEAR_COPIED
     got = host(r.run(x, w))
     assert r.device_status() == 0
     a, b = x[:, 7].contiguous(), w[:, 7].contiguous()
@@ -415,7 +415,7 @@ def test_low_halves_are_rounded(offset):
 
 
 # tensors that start off 16 bytes, fetched by copier warps: several work items to a CTA (a record of three SMs), so that the ring of stages goes on
-# from one to the next at every phase, and K loops shared by a cluster.  The form is the one that info names, or COPIED where that is TILES or PAIRS.
+# from one to the next at every phase, and K loops shared by a cluster.
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("sms,M,K,N", [(3, 70, 264, 1300), (3, 130, 1032, 900), (3, 33, 72, 2000), (148, 40, 4104, 500), (148, 12, 4104, 400)])
 def test_copiers_over_many_items_and_shared_loops(sms, M, K, N, dtype):
@@ -427,7 +427,7 @@ def test_copiers_over_many_items_and_shared_loops(sms, M, K, N, dtype):
         _, info = run_case(M, K, N, dtype, "relu", "after", pads=(8, 16, 1, 0), offset=1, seed=K)
     finally:
         B.mnn_set_calibration(before)
-    assert info.form in (B.LINEAR_TILES, B.LINEAR_PAIRS) and (info.items > sms if sms == 3 else info.split > 1)
+    assert info.form_unaligned == B.LINEAR_COPIED and (info.items > sms if sms == 3 else info.split > 1)
 
 
 def test_the_status_word_is_read_and_cleared():

@@ -88,6 +88,13 @@ def test_linear_plans():
                 assert i.split in (1, 2, 4, 8)
 
 
+def test_the_form_of_unaligned_starts_is_told():
+    assert linear(1, 4096, 4096, dtype="bf16").form_unaligned == B.LINEAR_FEW
+    for M, form in ((64, B.LINEAR_TILES), (8192, B.LINEAR_PAIRS)):
+        aligned, strides = linear(M, 4096, 4096, dtype="bf16"), linear(M, 4096, 4097, dtype="bf16")
+        assert aligned.form == strides.form == strides.form_unaligned == form and aligned.form_unaligned == B.LINEAR_COPIED
+
+
 # the record's number of SMs may be any positive number: plans on one SM have no pairs.  (In a process of their own: this once ended it.)
 @pytest.mark.parametrize("sms", [1, 2, 3, 148, 100000])
 def test_plans_for_any_number_of_sms(sms):
