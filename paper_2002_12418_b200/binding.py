@@ -465,7 +465,8 @@ def _raw_stream(device):
 class _OwnsWorkspace:
     """A runner's workspace, from torch's allocator.  The allocator gives memory that was freed to the next taker on the stream that it
     was allocated on, so it has to know of the other streams that use it: each is recorded at its first run.  A runner may then
-    be dropped behind a run on any stream.  (A captured graph is no stream: the runners whose runs it holds have to outlive it.)"""
+    be dropped behind a run on any stream.  (A captured graph is no stream: the runners whose runs it holds have to outlive it.  And
+    a stream that was not made by torch has to live until the runners that ran on it are dropped.)"""
     workspace = None
 
     def _allocate_workspace(self, nbytes: int, hand_over) -> None:
